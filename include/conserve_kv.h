@@ -347,6 +347,131 @@ int cs_kv_ckpt_load_run(const cs_kv_pool* pool, int32_t layer_begin, int32_t lay
                         const int32_t* page_ids, int32_t n, void* staging, size_t staging_bytes,
                         const cs_host_store* store, int32_t first_host_page, void* stream);
 
+/* ---- KV cache in 8 bits ----
+ * A pool whose K and V are e4m3 codes with one scale for each block: a page of 16 tokens, K or V, one
+ * kv head.  A code stands for code * scale; scales are powers of two, 2^-100 at least.  A page of a layer is
+ * half as long as in 16 bits, in bytes
+ *     [kv: 0 = K, 1 = V][kv_head][16 * head_dim] codes, then [kv][kv_head] scales (float),
+ * padded to a multiple of 16 (cs_kv8_page_bytes), so it moves as one blob: cs_kv_pages_copy is its
+ * checkpoint's gather and restore.  Inside a block (token t = 0..15 of the page, feature d), in bytes:
+ *     K:  ((d / 16) * 16 + t) * 16 + d % 16              [D/16][16 tokens][16 features]
+ *     V:  (((d / 64) * 4 + t / 4) * 16 + d % 16) * 16 + ((d / 16) % 4) * 4 + t % 4
+ *                                                        [D/64][4 token groups][16][4 feature tiles][4 tokens]
+ * Pages hold 16 tokens; batches, block tables and bad page ids are as for the 16-bit pools. */
+typedef struct {
+    void*   base;                   /* device, 16-byte aligned                           */
+    int32_t num_layers;
+    int32_t num_pages;
+    int32_t num_kv_heads;           /* at most 65535                                     */
+    int32_t head_dim;               /* 64 or 128                                         */
+    int64_t layer_stride;           /* BYTES, >= num_pages * page_stride, multiple of 16 */
+    int64_t page_stride;            /* BYTES, >= cs_kv8_page_bytes(), multiple of 16     */
+} cs_kv8_pool;
+
+/* Bytes of one (layer, page): codes, scales, padding.  0 if the shape is unsupported. */
+size_t cs_kv8_page_bytes(int32_t num_kv_heads, int32_t head_dim);
+
+/* cs_kv_append into an 8-bit pool: k_new, v_new (device [T][Hkv][D] bf16; fp16 in the _f16 call) are rounded
+ * to codes.  For each block that the step touches
+ *     e = the least exponent >= -100 with |x| <= 448 * 2^e for every new x of the block, and at least
+ *         the block's own exponent where it holds earlier tokens;   scale = 2^e
+ *     code = x / 2^e rounded to the nearest e4m3 value, ties to the even one
+ * and where e rises, the codes of the earlier tokens are divided by the rise and rounded again (exact
+ * unless they fall below 2^-6 of the new scale).  Pages that are full never change, slots behind the last
+ * token are left as they are, and a token's code depends only on its own value and its block's scale.
+ * Infinities do not count for e and end as the largest code; a NaN stays one.  fp16: values beyond 61440, the
+ * largest multiple of an e4m3 value that half precision holds, are rounded to it.  A block must not be appended to by two
+ * calls at once.  T == 0 is a no-op. */
+int cs_kv8_append(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch,
+                  const void* k_new, const void* v_new, void* stream);
+int cs_kv8_append_f16(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch,
+                      const void* k_new, const void* v_new, void* stream);
+
+/* cs_paged_attention_mixed over an 8-bit pool: K_s and V_s are code * scale, read through block_tables[s] and
+ * widened to the type of q and out (bf16; fp16 in the _f16 call) without rounding.  (Half precision: a value under 2^-14
+ * keeps what half precision has for it, and a scale whose codes pass 61440 is not one that cs_kv8_append_f16 makes.)
+ * Everything else is as there.  workspace: at least cs_paged_attention_kv8_workspace_bytes(). */
+size_t cs_paged_attention_kv8_workspace_bytes(const cs_batch* batch, int32_t num_q_heads,
+                                              int32_t num_kv_heads, int32_t head_dim);
+int cs_paged_attention_mixed_kv8(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch,
+                                 const void* q, void* out, int32_t num_q_heads,
+                                 float softmax_scale, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+int cs_paged_attention_mixed_kv8_f16(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch,
+                                     const void* q, void* out, int32_t num_q_heads,
+                                     float softmax_scale, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/* ---- Whole pages: copies, forks, frees, compaction ----
+ * A pool as pages of bytes, whatever is in them; from a 16- or an 8-bit pool by the calls below, or filled in by the
+ * caller: a contiguous staging buffer [layers][n][page bytes] is a space of n pages. */
+typedef struct {
+    void*   base;                   /* device, 16-byte aligned                           */
+    int32_t num_layers;
+    int32_t num_pages;
+    int64_t page_bytes;             /* multiple of 16, at most 2^30                      */
+    int64_t layer_stride;           /* BYTES, >= num_pages * page_stride (one layer: any), multiple of 16 */
+    int64_t page_stride;            /* BYTES, >= page_bytes, multiple of 16              */
+} cs_page_space;
+int cs_kv_page_space(const cs_kv_pool* pool, cs_page_space* space);
+int cs_kv8_page_space(const cs_kv8_pool* pool, cs_page_space* space);
+
+/* Copy: dst[dst_layer + l][dst_ids[i]] = src[src_layer + l][src_ids[i]] for 0 <= l < num_layers, 0 <= i < n.
+ * Ids: device [n], or NULL for 0, 1, .., n-1; a pair with an id outside its space is skipped.  src and dst have the
+ * same page_bytes and may be the same space.  Destinations must be distinct and none of them a source. */
+int cs_kv_pages_copy(const cs_page_space* src, int32_t src_layer, const int32_t* src_ids,
+                     const cs_page_space* dst, int32_t dst_layer, const int32_t* dst_ids,
+                     int32_t num_layers, int32_t n, void* stream);
+
+/* The block tables of the sequences that share a pool, with their lengths and, for each page, how many
+ * table entries hold it (0: free).  All of it lives on the device and is the caller's; row r holds its sequence's pages in
+ * its first ceil(lens[r] / page_size) entries.  A length beyond the row's entries counts as what they hold. */
+typedef struct {
+    int32_t* block_tables;          /* device [num_rows][max_blocks_per_seq]             */
+    int32_t* lens;                  /* device [num_rows], tokens                         */
+    int32_t* ref_counts;            /* device [num_pages]                                */
+    int32_t  num_rows;
+    int32_t  max_blocks_per_seq;
+    int32_t  num_pages;             /* of the pool                                       */
+    int32_t  page_size;             /* tokens of a page                                  */
+} cs_page_tables;
+
+/* Fork (samples of one prompt, beams): for 0 <= i < n, row children[i] becomes a sequence like row parents[i].
+ * Its first floor(len / page_size) pages are the parent's own (their counts go up by one); an unfinished last page is
+ * copied, layers layer_begin .. layer_end - 1, to page fresh_pages[i], whose count becomes 1, so that either may go on
+ * appending.  A parent whose length is a multiple of page_size needs none: fresh_pages[i] is not touched then.  The
+ * child's other entries become -1; what its row held before is NOT released (cs_kv_pages_free).
+ * parents, children, fresh_pages: device [n].  A parent may be named more often; children must be distinct and no
+ * parents, fresh pages distinct and free.  A fork with a row outside the tables is skipped; one that needs a fresh
+ * page and has none inside the pool makes a child of the full pages alone. */
+int cs_kv_pages_fork(const cs_page_space* space, int32_t layer_begin, int32_t layer_end,
+                     const cs_page_tables* tables, const int32_t* parents, const int32_t* children,
+                     const int32_t* fresh_pages, int32_t n, void* stream);
+
+/* Free: the rows rows[0 .. n) (device) give their pages back: each entry's count goes down by one, the entry
+ * becomes -1, the row's length 0.  The pages whose counts reach 0 are written to freed (device, room for num_pages) in
+ * ascending order, their number to *num_freed (device).  A row outside the tables is skipped, one listed twice freed
+ * once; the count of a page that is free already stays as it is. */
+int cs_kv_pages_free(const cs_page_tables* tables, const int32_t* rows, int32_t n,
+                     int32_t* freed, int32_t* num_freed, void* stream);
+
+/* Compaction: the pages with a count move to the front of the pool, so that everything from the number of
+ * them on can be given back.  With u pages in use, the k-th used page from page u on moves to the k-th free page below u, in
+ * layers layer_begin .. layer_end - 1 (a pool whose layers are compacted in parts takes the tables' results from one of
+ * the calls).  Written, all on the device:
+ *     new_ids[p]                  where page p went, -1 if it was free; num_pages entries
+ *     new_tables->block_tables    the tables under the new numbers, -1 behind a row's pages and for ids outside the pool
+ *     new_tables->ref_counts      the counts under the new numbers
+ *     *num_used                   u
+ * new_tables has the sizes of tables; its arrays may be the same ones, and its lens are not written.  Pages
+ * that moved keep their old contents too.  workspace: device, 16-byte aligned, at least
+ * cs_kv_pages_compact_workspace_bytes(); contents are scratch. */
+size_t cs_kv_pages_compact_workspace_bytes(int32_t num_pages);
+int cs_kv_pages_compact(const cs_page_space* space, int32_t layer_begin, int32_t layer_end,
+                        const cs_page_tables* tables, const cs_page_tables* new_tables,
+                        int32_t* new_ids, int32_t* num_used,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
 /* Plain device-to-device copy kernel of `bytes` (multiple of 16, both pointers 16-byte
  * aligned): the measured copy ceiling of the device and the calibration point for hardware
  * byte counters. */

@@ -68,6 +68,41 @@ class cs_safepoint(ctypes.Structure):
     ]
 
 
+class cs_kv8_pool(ctypes.Structure):
+    _fields_ = [
+        ("base", ctypes.c_void_p),
+        ("num_layers", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("layer_stride", ctypes.c_int64),
+        ("page_stride", ctypes.c_int64),
+    ]
+
+
+class cs_page_space(ctypes.Structure):
+    _fields_ = [
+        ("base", ctypes.c_void_p),
+        ("num_layers", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("page_bytes", ctypes.c_int64),
+        ("layer_stride", ctypes.c_int64),
+        ("page_stride", ctypes.c_int64),
+    ]
+
+
+class cs_page_tables(ctypes.Structure):
+    _fields_ = [
+        ("block_tables", ctypes.c_void_p),
+        ("lens", ctypes.c_void_p),
+        ("ref_counts", ctypes.c_void_p),
+        ("num_rows", ctypes.c_int32),
+        ("max_blocks_per_seq", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+    ]
+
+
 class CsError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -122,6 +157,21 @@ def lib():
                                     ctypes.POINTER(ctypes.c_int32), vp]
         L.cs_run_layers_workspace_bytes.restype = sz
         L.cs_run_layers_workspace_bytes.argtypes = [BP, i32, i32, i32, i32]
+        P8, SP, TP = ctypes.POINTER(cs_kv8_pool), ctypes.POINTER(cs_page_space), ctypes.POINTER(cs_page_tables)
+        L.cs_kv8_page_bytes.restype, L.cs_kv8_page_bytes.argtypes = sz, [i32, i32]
+        for f in (L.cs_kv8_append, L.cs_kv8_append_f16):
+            f.restype, f.argtypes = ctypes.c_int, [P8, i32, BP, vp, vp, vp]
+        L.cs_paged_attention_kv8_workspace_bytes.restype = sz
+        L.cs_paged_attention_kv8_workspace_bytes.argtypes = [BP, i32, i32, i32]
+        for f in (L.cs_paged_attention_mixed_kv8, L.cs_paged_attention_mixed_kv8_f16):
+            f.restype, f.argtypes = ctypes.c_int, [P8, i32, BP, vp, vp, i32, ctypes.c_float, vp, sz, vp]
+        L.cs_kv_page_space.restype, L.cs_kv_page_space.argtypes = ctypes.c_int, [PP, SP]
+        L.cs_kv8_page_space.restype, L.cs_kv8_page_space.argtypes = ctypes.c_int, [P8, SP]
+        L.cs_kv_pages_copy.restype, L.cs_kv_pages_copy.argtypes = ctypes.c_int, [SP, i32, vp, SP, i32, vp, i32, i32, vp]
+        L.cs_kv_pages_fork.restype, L.cs_kv_pages_fork.argtypes = ctypes.c_int, [SP, i32, i32, TP, vp, vp, vp, i32, vp]
+        L.cs_kv_pages_free.restype, L.cs_kv_pages_free.argtypes = ctypes.c_int, [TP, vp, i32, vp, vp, vp]
+        L.cs_kv_pages_compact_workspace_bytes.restype, L.cs_kv_pages_compact_workspace_bytes.argtypes = sz, [i32]
+        L.cs_kv_pages_compact.restype, L.cs_kv_pages_compact.argtypes = ctypes.c_int, [SP, i32, i32, TP, TP, vp, vp, vp, sz, vp]
         L.cs_debug_set_cu_count.restype, L.cs_debug_set_cu_count.argtypes = None, [i32]
         L.cs_debug_copy.restype, L.cs_debug_copy.argtypes = ctypes.c_int, [vp, vp, sz, vp]
         L.cs_set_decode_split_tokens.restype, L.cs_set_decode_split_tokens.argtypes = None, [i32]
@@ -152,7 +202,10 @@ EXPORTS = [
     "cs_kv_ckpt_restore_tokens", "cs_kv_ckpt_save",
     "cs_kv_ckpt_load", "cs_kv_ckpt_save_run", "cs_kv_ckpt_load_run", "cs_page_map_create", "cs_page_map_destroy",
     "cs_page_map_host_of", "cs_page_map_gpu_of", "cs_page_map_free_host_pages", "cs_page_map_checkpoint",
-    "cs_page_map_evict", "cs_page_map_bind", "cs_page_map_drop", "cs_run_layers", "cs_run_layers_f16", "cs_run_layers_workspace_bytes", "cs_debug_set_cu_count", "cs_debug_copy", "cs_debug_decode_items", "cs_debug_decode_pages_ahead", "cs_debug_decode_loads", "cs_debug_prefill_order",
+    "cs_page_map_evict", "cs_page_map_bind", "cs_page_map_drop", "cs_run_layers", "cs_run_layers_f16", "cs_run_layers_workspace_bytes",
+    "cs_kv8_page_bytes", "cs_kv8_append", "cs_kv8_append_f16", "cs_paged_attention_kv8_workspace_bytes", "cs_paged_attention_mixed_kv8",
+    "cs_paged_attention_mixed_kv8_f16", "cs_kv_page_space", "cs_kv8_page_space", "cs_kv_pages_copy", "cs_kv_pages_fork", "cs_kv_pages_free",
+    "cs_kv_pages_compact", "cs_kv_pages_compact_workspace_bytes", "cs_debug_set_cu_count", "cs_debug_copy", "cs_debug_decode_items", "cs_debug_decode_pages_ahead", "cs_debug_decode_loads", "cs_debug_prefill_order",
     "cs_set_decode_split_tokens", "cs_set_decode_pages_ahead", "cs_set_mixed_fusion", "cs_debug_mixed_arrangement", "cs_debug_mixed_tile_priority", "cs_debug_mixed_tail_cut", "cs_debug_set_tail_cut", "cs_debug_play_tiles", "cs_status_string", "cs_last_hip_error",
 ]
 
@@ -191,6 +244,58 @@ class Pool:
     def empty(cls, L, P, Hkv, D, device="cuda", page_size: int = PAGE):
         t = torch.empty((L, P, 2, Hkv, page_size * D), dtype=torch.bfloat16, device=device)
         return cls(t, L, P, Hkv, D, page_size=page_size)
+
+
+class Pool8:
+    """A cs_kv8_pool over a uint8 torch tensor [L, P, page_stride] (or any tensor of that many bytes); keeps the
+    tensor alive.  Strides are in bytes."""
+
+    def __init__(self, tensor: torch.Tensor, L: int, P: int, Hkv: int, D: int,
+                 layer_stride: Optional[int] = None, page_stride: Optional[int] = None):
+        self.tensor = tensor
+        self.page_bytes = cs_kv8_page_bytes(Hkv, D)
+        self.page_stride = self.page_bytes if page_stride is None else page_stride
+        self.layer_stride = P * self.page_stride if layer_stride is None else layer_stride
+        self.c = cs_kv8_pool(_ptr(tensor), L, P, Hkv, D, self.layer_stride, self.page_stride)
+        self.L, self.P, self.Hkv, self.D = L, P, Hkv, D
+
+    @classmethod
+    def empty(cls, L, P, Hkv, D, device="cuda"):
+        """Pages at multiples of 128 bytes, the cache line."""
+        stride = (cs_kv8_page_bytes(Hkv, D) + 127) // 128 * 128
+        return cls(torch.empty((L, P, stride), dtype=torch.uint8, device=device), L, P, Hkv, D, page_stride=stride)
+
+
+class PageSpace:
+    """A cs_page_space: a pool (Pool or Pool8) as pages of bytes; keeps its tensor alive."""
+
+    def __init__(self, tensor: torch.Tensor, c: cs_page_space):
+        self.tensor, self.c = tensor, c
+
+    @classmethod
+    def of(cls, pool):
+        c = cs_page_space()
+        fn = lib().cs_kv8_page_space if isinstance(pool, Pool8) else lib().cs_kv_page_space
+        _check(fn(ctypes.byref(pool.c), ctypes.byref(c)), "cs_kv_page_space")
+        return cls(pool.tensor, c)
+
+    @classmethod
+    def staging(cls, tensor: torch.Tensor):
+        """A contiguous tensor [layers, n, ...] as a space of n pages."""
+        assert tensor.is_contiguous() and tensor.dim() >= 3
+        page = tensor[0, 0].numel() * tensor.element_size()
+        return cls(tensor, cs_page_space(_ptr(tensor), int(tensor.shape[0]), int(tensor.shape[1]), page, int(tensor.shape[1]) * page, page))
+
+
+class PageTables:
+    """A cs_page_tables over device int32 tensors [rows, blocks], [rows], [pages]; keeps them alive."""
+
+    def __init__(self, block_tables: torch.Tensor, lens: torch.Tensor, ref_counts: torch.Tensor, page_size: int = PAGE):
+        assert block_tables.dim() == 2 and lens.shape == block_tables.shape[:1] and ref_counts.dim() == 1
+        assert all(t.dtype == torch.int32 and t.is_contiguous() for t in (block_tables, lens, ref_counts))
+        self.block_tables, self.lens, self.ref_counts = block_tables, lens, ref_counts
+        self.c = cs_page_tables(_ptr(block_tables), _ptr(lens), _ptr(ref_counts), int(block_tables.shape[0]), int(block_tables.shape[1]),
+                                int(ref_counts.numel()), page_size)
 
 
 class Batch:
@@ -441,6 +546,79 @@ def run_layers_workspace_for(batch: Batch, num_online_seqs: int, Hq: int, Hkv: i
     if n:                                               # room for the four layers that share a launch, if that is little
         n = max(n, min(4 * n + n // 8 + 256, 64 << 20))
     return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+
+
+def cs_kv8_page_bytes(Hkv: int, D: int) -> int:
+    return int(lib().cs_kv8_page_bytes(Hkv, D))
+
+
+def cs_kv8_append(pool: Pool8, layer: int, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor, stream=None):
+    _check(lib().cs_kv8_append(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _ptr(k_new), _ptr(v_new),
+                               _stream(stream)), "cs_kv8_append")
+
+
+def cs_kv8_append_f16(pool: Pool8, layer: int, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor, stream=None):
+    _check(lib().cs_kv8_append_f16(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _ptr(k_new), _ptr(v_new),
+                                   _stream(stream)), "cs_kv8_append_f16")
+
+
+def cs_paged_attention_kv8_workspace_bytes(batch: Batch, Hq: int, Hkv: int, D: int) -> int:
+    return int(lib().cs_paged_attention_kv8_workspace_bytes(ctypes.byref(batch.c), Hq, Hkv, D))
+
+
+def workspace_for_kv8(batch: Batch, Hq: int, Hkv: int, D: int, device="cuda") -> torch.Tensor:
+    n = cs_paged_attention_kv8_workspace_bytes(batch, Hq, Hkv, D)
+    return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+
+
+def cs_paged_attention_mixed_kv8(pool: Pool8, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor,
+                                 Hq: int, softmax_scale: float, workspace: Optional[torch.Tensor], stream=None):
+    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().cs_paged_attention_mixed_kv8(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _ptr(q), _ptr(out),
+                                              Hq, softmax_scale, _ptr(workspace), wb, _stream(stream)),
+           "cs_paged_attention_mixed_kv8")
+
+
+def cs_paged_attention_mixed_kv8_f16(pool: Pool8, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor,
+                                     Hq: int, softmax_scale: float, workspace: Optional[torch.Tensor], stream=None):
+    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().cs_paged_attention_mixed_kv8_f16(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _ptr(q), _ptr(out),
+                                                  Hq, softmax_scale, _ptr(workspace), wb, _stream(stream)),
+           "cs_paged_attention_mixed_kv8_f16")
+
+
+def cs_kv_pages_copy(src: PageSpace, src_layer: int, src_ids: Optional[torch.Tensor], dst: PageSpace, dst_layer: int,
+                     dst_ids: Optional[torch.Tensor], num_layers: int, n: Optional[int] = None, stream=None):
+    """n: by default the length of the id lists; needed where both are None."""
+    if n is None:
+        n = (src_ids if src_ids is not None else dst_ids).numel()
+    _check(lib().cs_kv_pages_copy(ctypes.byref(src.c), src_layer, _ptr(src_ids), ctypes.byref(dst.c), dst_layer, _ptr(dst_ids),
+                                  num_layers, n, _stream(stream)), "cs_kv_pages_copy")
+
+
+def cs_kv_pages_fork(space: PageSpace, layer_begin: int, layer_end: int, tables: PageTables, parents: torch.Tensor,
+                     children: torch.Tensor, fresh_pages: torch.Tensor, stream=None):
+    assert parents.numel() == children.numel() == fresh_pages.numel()
+    _check(lib().cs_kv_pages_fork(ctypes.byref(space.c), layer_begin, layer_end, ctypes.byref(tables.c), _ptr(parents), _ptr(children),
+                                  _ptr(fresh_pages), parents.numel(), _stream(stream)), "cs_kv_pages_fork")
+
+
+def cs_kv_pages_free(tables: PageTables, rows: torch.Tensor, freed: torch.Tensor, num_freed: torch.Tensor, stream=None):
+    assert freed.numel() >= tables.ref_counts.numel()
+    _check(lib().cs_kv_pages_free(ctypes.byref(tables.c), _ptr(rows), rows.numel(), _ptr(freed), _ptr(num_freed), _stream(stream)),
+           "cs_kv_pages_free")
+
+
+def cs_kv_pages_compact(space: PageSpace, layer_begin: int, layer_end: int, tables: PageTables, new_tables: PageTables,
+                        new_ids: torch.Tensor, num_used: torch.Tensor, workspace: torch.Tensor, stream=None):
+    assert new_ids.numel() >= tables.ref_counts.numel()
+    _check(lib().cs_kv_pages_compact(ctypes.byref(space.c), layer_begin, layer_end, ctypes.byref(tables.c), ctypes.byref(new_tables.c),
+                                     _ptr(new_ids), _ptr(num_used), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                     _stream(stream)), "cs_kv_pages_compact")
+
+
+def compact_workspace_for(space: PageSpace, device="cuda") -> torch.Tensor:
+    return torch.empty(int(lib().cs_kv_pages_compact_workspace_bytes(space.c.num_pages)), dtype=torch.uint8, device=device)
 
 
 def cs_debug_set_cu_count(cus: int):

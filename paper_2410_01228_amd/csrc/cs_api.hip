@@ -97,7 +97,7 @@ static int32_t item_keys(const cs_batch* b, uint32_t w) {
 // How the decode kernel loads its pages in a launch of `layers` layers: pages_ahead, counted_loads.
 static void plan_decode_loads(const cs_batch* b, DecodePlan& p, int32_t Hkv, int32_t head_dim, int32_t layers) {
     const int64_t cus = device_cus(), wgs = (int64_t)p.total_items * Hkv * layers;
-    const int64_t kv_bytes = p.decode_keys * 2 * Hkv * head_dim * 2 * layers;
+    const int64_t kv_bytes = p.decode_keys * 2 * Hkv * head_dim * p.elem_bytes * layers;
     // Two pages ahead per wavefront need the registers of the third workgroup per CU.  Measured
     // over 33 batch shapes: the deeper queue wins 2-6% once the launch is long enough for the
     // steady state to dominate (from about 0.65 GB of K/V on, ~100 us), and loses 2-7% on
@@ -141,8 +141,9 @@ static void plan_decode_loads(const cs_batch* b, DecodePlan& p, int32_t Hkv, int
     }
 }
 
-DecodePlan plan_decode(const cs_batch* b, int32_t Hkv, int32_t head_dim) {
+DecodePlan plan_decode(const cs_batch* b, int32_t Hkv, int32_t head_dim, int32_t elem_bytes) {
     DecodePlan p = {};
+    p.elem_bytes = elem_bytes;
     int32_t max_keys = 0, min_keys = 2147483647;
     for (int32_t s = 0; s < b->num_seqs; ++s) {
         const int32_t ql = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s];
@@ -176,7 +177,7 @@ DecodePlan plan_decode(const cs_batch* b, int32_t Hkv, int32_t head_dim) {
         // 3.8% -> 2.3%, worst 61% -> 17%, together with the floor rule below).
         // (the workgroup counts and byte volumes below were measured on 256 CUs and scale with the chip)
         const int32_t cap = head_dim >= 128 ? 4096 : 8192;
-        const int64_t kv_bytes = p.decode_keys * 2 * Hkv * head_dim * 2;
+        const int64_t kv_bytes = p.decode_keys * 2 * Hkv * head_dim * elem_bytes;
         const int64_t need = p.uniform ? cus : kv_bytes >= 400000000ll * cus / 256 ? 3 * cus : cus * 3 / 2;
         auto workgroups_at = [&](int32_t sp) {
             int64_t items = 0;
@@ -481,7 +482,7 @@ static FusePlan plan_fusion_by_model(const cs_batch* b, const DecodePlan& d, Pre
     }
     // ideal times: flops at 1 PFLOP/s, bytes at 6 TB/s
     const double t_prefill = 4.0 * Hq * D * pairs / 1.0e15;
-    const double decode_bytes = (double)d.decode_keys * 2 * Hkv * D * 2;
+    const double decode_bytes = (double)d.decode_keys * 2 * Hkv * D * d.elem_bytes;
     const double t_decode = decode_bytes / 6.0e12;
     // Behind the tiles, where nothing below says otherwise: over 853 mixes of four model shapes two
     // kernels in a row are 15% slower in the geometric mean than the better of the two grids, and more
@@ -696,7 +697,7 @@ static bool decode_merges_in_place(const DecodePlan& d, const PrefillPlan& p, co
 // 0.4% and 11%.
 static bool tiles_merge_in_place(const DecodePlan& d, const PrefillPlan& p, const FusePlan& f, int32_t Hkv, int32_t D, int32_t layers) {
     if (f.arrangement == 0 || p.max_ranges <= 1) return false;
-    const double t_decode = (double)layers * d.decode_keys * 2 * Hkv * D * 2 / 6.5e6, t_range = 0.88 * p.range_steps;    // microseconds
+    const double t_decode = (double)layers * d.decode_keys * 2 * Hkv * D * d.elem_bytes / 6.5e6, t_range = 0.88 * p.range_steps;    // microseconds
     return p.max_ranges == 2 || t_decode >= 0.7 * t_range;
 }
 
@@ -769,7 +770,7 @@ extern "C" {
 // compared value by value.
 struct PlanMemo {
     bool valid = false;
-    int32_t S = 0, T = 0, Hq = 0, Hkv = 0, D = 0, layers = 0, split = 0, ahead = 0, cus = 0, fuse = 0, tail_whole = -1, tail_ranges = 0;
+    int32_t S = 0, T = 0, Hq = 0, Hkv = 0, D = 0, layers = 0, split = 0, ahead = 0, cus = 0, fuse = 0, tail_whole = -1, tail_ranges = 0, elem_bytes = 2;
     std::vector<int32_t> ctx, cu;
     Plans plans;
 };
@@ -777,8 +778,8 @@ struct PlanMemo {
 
 namespace cs {
 // One layer's plan.
-static void plan_layer(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D, int32_t fuse, Plans& plans) {
-    plans.d = plan_decode(b, Hkv, D);
+static void plan_layer(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D, int32_t elem_bytes, int32_t fuse, Plans& plans) {
+    plans.d = plan_decode(b, Hkv, D, elem_bytes);
     plans.p = plans.d.num_prefill ? plan_prefill(b, Hq, Hkv, D, 1) : PrefillPlan{};
     plans.f = plan_fusion(b, plans.d, plans.p, Hq, Hkv, D, fuse);
 }
@@ -794,7 +795,7 @@ static void plan_for_layers(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t 
     plans.p.bytes *= layers;
 }
 
-const Plans& plans_for(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D, int32_t layers) {
+const Plans& plans_for(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D, int32_t layers, int32_t elem_bytes) {
     constexpr int kMemos = 6;
     static thread_local PlanMemo memo[kMemos];
     static thread_local int next = 0;
@@ -802,12 +803,12 @@ const Plans& plans_for(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D, in
     const int32_t fuse = g_fuse_mixed.load(), tail_whole = g_forced_tail_whole.load(), tail_ranges = g_forced_tail_ranges.load();
     for (PlanMemo& m : memo)
         if (m.valid && m.fuse == fuse && m.tail_whole == tail_whole && m.tail_ranges == tail_ranges && m.S == S && m.T == b->num_tokens && m.Hq == Hq && m.Hkv == Hkv && m.D == D &&
-            m.layers == layers && m.split == split && m.ahead == ahead && m.cus == cus &&
+            m.layers == layers && m.elem_bytes == elem_bytes && m.split == split && m.ahead == ahead && m.cus == cus &&
             memcmp(m.ctx.data(), b->h_ctx_lens, sizeof(int32_t) * S) == 0 && memcmp(m.cu.data(), b->h_cu_q_lens, sizeof(int32_t) * (S + 1)) == 0)
             return m.plans;
     Plans plans;
-    if (layers > 1) plans = plans_for(b, Hq, Hkv, D, 1);
-    else plan_layer(b, Hq, Hkv, D, fuse, plans);
+    if (layers > 1) plans = plans_for(b, Hq, Hkv, D, 1, elem_bytes);
+    else plan_layer(b, Hq, Hkv, D, elem_bytes, fuse, plans);
     if (layers > 1) plan_for_layers(b, Hq, Hkv, D, fuse, layers, plans);
     plans.d.merges_in_place = decode_merges_in_place(plans.d, plans.p, plans.f, Hkv, D, layers);
     plans.p.merges_in_place = tiles_merge_in_place(plans.d, plans.p, plans.f, Hkv, D, layers);
@@ -824,7 +825,7 @@ const Plans& plans_for(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D, in
     PlanMemo& m = memo[next];
     next = (next + 1) % kMemos;
     m.valid = false;
-    m.S = S; m.T = b->num_tokens; m.Hq = Hq; m.Hkv = Hkv; m.D = D; m.layers = layers; m.split = split; m.ahead = ahead; m.cus = cus; m.fuse = fuse; m.tail_whole = tail_whole; m.tail_ranges = tail_ranges;
+    m.S = S; m.T = b->num_tokens; m.Hq = Hq; m.Hkv = Hkv; m.D = D; m.layers = layers; m.elem_bytes = elem_bytes; m.split = split; m.ahead = ahead; m.cus = cus; m.fuse = fuse; m.tail_whole = tail_whole; m.tail_ranges = tail_ranges;
     m.ctx.assign(b->h_ctx_lens, b->h_ctx_lens + S);
     m.cu.assign(b->h_cu_q_lens, b->h_cu_q_lens + S + 1);
     m.plans = plans;

@@ -108,6 +108,7 @@ struct DecodePlan {
     int32_t total_items;       // sum over decode sequences of their split count
     int32_t num_multi;         // decode sequences cut into more than one item
     int64_t decode_keys;       // total keys read by decode sequences
+    int32_t elem_bytes;        // of an element of K and V: 2, or 1 in an 8-bit pool
     bool    uniform;           // their lengths lie within 25% of each other
     int32_t longest;           // keys of the longest work item
     int32_t max_pieces;        // items of the sequence that is cut into most
@@ -117,7 +118,7 @@ struct DecodePlan {
     bool    merges_in_place;   // the workgroups merge the cut sequences themselves, no kernel follows
     ItemsInArgs arg_items;     // total_items words
 };
-DecodePlan plan_decode(const cs_batch* batch, int32_t num_kv_heads, int32_t head_dim);
+DecodePlan plan_decode(const cs_batch* batch, int32_t num_kv_heads, int32_t head_dim, int32_t elem_bytes = 2);
 // Workspace layout (all 16-byte aligned): announcements of the partials (where they are merged in
 // place: 8 bytes per item and kv head, cs_arrive.h) or, unless it travels in the kernel arguments, the item
 // list | partial (max, sum) | partial outputs.  All zero when nothing is cut.
@@ -199,5 +200,15 @@ int launch_mixed_layers(const cs_kv_pool& pool, int32_t layer, const LayerSpan& 
                         const PrefillPlan& pplan, const void* q, void* out, int32_t Hq, float scale,
                         void* decode_workspace_base, void* prefill_workspace, hipStream_t st, bool f16,
                         int32_t tile_priority, int32_t persistent_wgs);
+
+// The same over a pool of 8-bit codes, one layer: `pool` is its view in 16-bit units (kv8_view), f16 the type of q
+// and out.
+int launch_decode_kv8(const cs_kv_pool& pool, int32_t layer, const cs_batch& b, const DecodePlan& plan, const void* q, void* out,
+                      int32_t Hq, float scale, void* workspace, hipStream_t st, bool f16, bool merge_only);
+int launch_prefill_kv8(const cs_kv_pool& pool, int32_t layer, const cs_batch& b, const PrefillPlan& plan, const void* q, void* out,
+                       int32_t Hq, float scale, void* workspace, hipStream_t st, bool f16);
+int launch_mixed_kv8(const cs_kv_pool& pool, int32_t layer, const cs_batch& b, const DecodePlan& dplan, const PrefillPlan& pplan,
+                     const void* q, void* out, int32_t Hq, float scale, void* decode_workspace_base, void* prefill_workspace,
+                     hipStream_t st, bool f16, int32_t tile_priority, int32_t persistent_wgs);
 
 }  // namespace cs

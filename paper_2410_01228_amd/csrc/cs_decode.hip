@@ -1,6 +1,7 @@
 // Kernels and launcher of the decode path (the workgroup's work itself is in
 // cs_decode_impl.h, shared with the fused mixed-batch kernel).
 #include "cs_decode_impl.h"
+#include "cs_decode8_impl.h"
 
 namespace cs {
 
@@ -68,7 +69,11 @@ __device__ __forceinline__ void split_workgroup(
     const int32_t item = blockIdx.x / Hkv, g = blockIdx.x - item * Hkv, n_items = gridDim.x / Hkv;
     const DecodePartials mine = part.of_layer(blockIdx.y, n_items, Hkv * G, Hkv, D);
     out += blockIdx.y * next_q;
-    decode_item<D, Src, E, kAhead, PS, kLoads>(lds, layer_base + blockIdx.y * next_layer, page_stride, num_pages, Hkv, G, block_tables, max_blocks, src, ctx_lens,
+    if constexpr (E::kEightBit)
+        decode_item8<D, Src, E, kAhead, kLoads>(lds, layer_base + blockIdx.y * next_layer, page_stride, num_pages, Hkv, G, block_tables, max_blocks, src, ctx_lens,
+                           cu_q_lens, q + blockIdx.y * next_q, out, scale_log2e, mine, item, g);
+    else
+        decode_item<D, Src, E, kAhead, PS, kLoads>(lds, layer_base + blockIdx.y * next_layer, page_stride, num_pages, Hkv, G, block_tables, max_blocks, src, ctx_lens,
                            cu_q_lens, q + blockIdx.y * next_q, out, scale_log2e, mine, item, g);
     if constexpr (kCut) {
         if (part.words) merge_in_place<D, E>(lds, mine, src, item, g, ctx_lens, cu_q_lens, Hkv, G, out);
@@ -125,6 +130,7 @@ static int launch_decode_as(const cs_kv_pool& pool, int32_t layer, const LayerSp
                             bool merge_only)
 {
     if (plan.num_decode == 0) return CS_OK;
+    constexpr int kOtherPage = E::kEightBit ? 16 : 8;                  // (8-bit pools have pages of 16 only)
     const int32_t Hkv = pool.num_kv_heads, D = pool.head_dim, G = Hq / Hkv;
     const uint16_t* layer_base = (const uint16_t*)pool.base + (int64_t)layer * pool.layer_stride;
     const float scale_log2e = scale * 1.4426950408889634f;
@@ -141,13 +147,13 @@ static int launch_decode_as(const cs_kv_pool& pool, int32_t layer, const LayerSp
                        src, b.ctx_lens, b.cu_q_lens, (const uint16_t*)q, (uint16_t*)out,               \
                        scale_log2e, part, span.pool, span.q);
 #define CS_LAUNCH_DECODE_A(KERNEL, DD, SRC, src, AH, CUT)                                                    \
-    if (pool.page_size == 16) { CS_LAUNCH_DECODE_P(KERNEL, DD, SRC, src, AH, 16, CUT) } else { CS_LAUNCH_DECODE_P(KERNEL, DD, SRC, src, AH, 8, CUT) }
+    if (pool.page_size == 16) { CS_LAUNCH_DECODE_P(KERNEL, DD, SRC, src, AH, 16, CUT) } else { CS_LAUNCH_DECODE_P(KERNEL, DD, SRC, src, AH, kOtherPage, CUT) }
 #define CS_LAUNCH_DECODE(KERNEL, DD, SRC, src, CUT)                                                         \
     if (plan.pages_ahead == 2) { CS_LAUNCH_DECODE_A(KERNEL, DD, SRC, src, 2, CUT) } else { CS_LAUNCH_DECODE_A(KERNEL, DD, SRC, src, 1, CUT) }
 #define CS_LAUNCH_DECODE_ARGS(DD, CUT)                                                                      \
     if (plan.counted_loads) { CS_LAUNCH_DECODE(decode_lone_kernel, DD, ItemsInArgs, plan.arg_items, CUT) } else { CS_LAUNCH_DECODE(decode_split_kernel, DD, ItemsInArgs, plan.arg_items, CUT) }
 #define CS_LAUNCH_MERGE(DD, SRC, src)                                                                       \
-    hipLaunchKernelGGL((decode_merge_kernel<DD, SRC, E>), grid, dim3(kDecodeThreads), 0, st, Hkv, G, src, b.ctx_lens, \
+    hipLaunchKernelGGL((decode_merge_kernel<DD, SRC, typename E::Wide>), grid, dim3(kDecodeThreads), 0, st, Hkv, G, src, b.ctx_lens, \
                        b.cu_q_lens, (uint16_t*)out, part, span.q);
     if (plan.in_args) {
         // (merge_only: the fused mixed-batch kernel has already done the items' work)
@@ -193,6 +199,14 @@ int launch_decode(const cs_kv_pool& pool, int32_t layer, const cs_batch& b, cons
                   bool merge_only)
 {
     return launch_decode_layers(pool, layer, LayerSpan{1, 0, 0, 0}, b, plan, q, out, Hq, scale, workspace, st, f16, merge_only);
+}
+
+int launch_decode_kv8(const cs_kv_pool& pool, int32_t layer, const cs_batch& b, const DecodePlan& plan, const void* q, void* out,
+                      int32_t Hq, float scale, void* workspace, hipStream_t st, bool f16, bool merge_only)
+{
+    const LayerSpan one = {1, 0, 0, 0};
+    return f16 ? launch_decode_as<Kv8<F16>>(pool, layer, one, b, plan, q, out, Hq, scale, workspace, st, merge_only)
+               : launch_decode_as<Kv8<Bf16>>(pool, layer, one, b, plan, q, out, Hq, scale, workspace, st, merge_only);
 }
 
 }  // namespace cs

@@ -294,6 +294,60 @@ __device__ __forceinline__ void merge_pieces(const DecodePartials& part, int32_t
     }
 }
 
+// The end of decode_item: merges the four wavefronts' states through LDS and writes the output rows, or, for a piece
+// of a cut sequence, its partial.
+template <int D, class E>
+__device__ __forceinline__ void leave_item(
+    DecodeLds<D>& lds, WaveState<D>& st, const DecodeItem& it, int32_t t, int32_t item, int32_t g, int32_t Hq, int32_t G,
+    uint16_t* __restrict__ out, const DecodePartials& part, int lane, int wave)
+{
+    st.l += __shfl_xor(st.l, 16, 64);
+    st.l += __shfl_xor(st.l, 32, 64);
+
+    // merge the four wavefronts through LDS
+    auto& sh_o = lds.o;
+    auto& sh_m = lds.m;
+    auto& sh_l = lds.l;
+    {
+        const int head = lane & 15;
+        if (head < G) {
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sh_o[wave][head][dt * 16 + (lane >> 4) * 4 + i] = st.o[dt][i];
+            if (lane < 16) { sh_m[wave][head] = st.m; sh_l[wave][head] = st.l; }
+        }
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < G * D; idx += kDecodeThreads) {
+        const int head = idx / D, d = idx - head * D;
+        float M = sh_m[0][head];
+#pragma unroll
+        for (int w = 1; w < kDecodeWaves; ++w) M = fmaxf(M, sh_m[w][head]);
+        float L = 0.f, O = 0.f;
+#pragma unroll
+        for (int w = 0; w < kDecodeWaves; ++w) {
+            const float mw = sh_m[w][head];
+            const float f = mw == -INFINITY ? 0.f : exp2f(mw - M);     // a wavefront without pages
+            L += sh_l[w][head] * f;
+            O += sh_o[w][head][d] * f;
+        }
+        const int32_t hq = g * G + head;
+        if (it.n_splits == 1) {
+            const float r = L > 0.f ? O / L : 0.f;                    // no key at all (every page id bad): zeros
+            out[((int64_t)t * Hq + hq) * D + d] = (uint16_t)(E::pack(r, 0.f) & 0xffffu);
+        } else {
+            const int64_t slot = (int64_t)item * Hq + hq;
+            __hip_atomic_store(part.o + slot * D + d, O, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (d == 0) {
+                __hip_atomic_store(part.ml + slot * 2, M, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(part.ml + slot * 2 + 1, L, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+    }
+}
+
 // How a wavefront of decode_item loads its pages, and what it does about a step without one (past the end of the
 // range, or a bad id).
 // kSkipped: the loads of such a step are skipped.  The compiler cannot count loads behind a branch, so it waits for
@@ -421,51 +475,7 @@ __device__ __forceinline__ void decode_item(
             stage(b2, b1);
         }
     }
-    st.l += __shfl_xor(st.l, 16, 64);
-    st.l += __shfl_xor(st.l, 32, 64);
-
-    // merge the four wavefronts through LDS
-    auto& sh_o = lds.o;
-    auto& sh_m = lds.m;
-    auto& sh_l = lds.l;
-    {
-        const int head = lane & 15;
-        if (head < G) {
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    sh_o[wave][head][dt * 16 + (lane >> 4) * 4 + i] = st.o[dt][i];
-            if (lane < 16) { sh_m[wave][head] = st.m; sh_l[wave][head] = st.l; }
-        }
-    }
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < G * D; idx += kDecodeThreads) {
-        const int head = idx / D, d = idx - head * D;
-        float M = sh_m[0][head];
-#pragma unroll
-        for (int w = 1; w < kDecodeWaves; ++w) M = fmaxf(M, sh_m[w][head]);
-        float L = 0.f, O = 0.f;
-#pragma unroll
-        for (int w = 0; w < kDecodeWaves; ++w) {
-            const float mw = sh_m[w][head];
-            const float f = mw == -INFINITY ? 0.f : exp2f(mw - M);     // a wavefront without pages
-            L += sh_l[w][head] * f;
-            O += sh_o[w][head][d] * f;
-        }
-        const int32_t hq = g * G + head;
-        if (it.n_splits == 1) {
-            const float r = L > 0.f ? O / L : 0.f;                    // no key at all (every page id bad): zeros
-            out[((int64_t)t * Hq + hq) * D + d] = (uint16_t)(E::pack(r, 0.f) & 0xffffu);
-        } else {
-            const int64_t slot = (int64_t)item * Hq + hq;
-            __hip_atomic_store(part.o + slot * D + d, O, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (d == 0) {
-                __hip_atomic_store(part.ml + slot * 2, M, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __hip_atomic_store(part.ml + slot * 2 + 1, L, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-        }
-    }
+    leave_item<D, E>(lds, st, it, t, item, g, Hq, G, out, part, lane, wave);
 }
 
 // The end of a workgroup that has worked off item `item` and kv head g: if that is a piece of a cut

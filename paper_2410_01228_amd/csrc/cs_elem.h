@@ -14,6 +14,13 @@ typedef uint32_t e_u32x2 __attribute__((ext_vector_type(2)));
 typedef float e_f32x4 __attribute__((ext_vector_type(4)));
 
 struct Bf16 {
+    typedef Bf16 Wide;
+    static constexpr bool kEightBit = false;
+    // two e4m3 codes of a dword (the lower or the upper half) times a power of two, exactly
+    template <bool kUpper> static __device__ __forceinline__ uint32_t widen(uint32_t codes, float scale) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, kUpper));
+    }
+    static constexpr uint32_t kInfinity = 0x7f80u;                 // a half-word above it, sign aside, is no number
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef short s4 __attribute__((ext_vector_type(4)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
@@ -45,6 +52,12 @@ struct Bf16 {
 };
 
 struct F16 {
+    typedef F16 Wide;
+    static constexpr bool kEightBit = false;
+    template <bool kUpper> static __device__ __forceinline__ uint32_t widen(uint32_t codes, float scale) {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, kUpper));
+    }
+    static constexpr uint32_t kInfinity = 0x7c00u;
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     typedef _Float16 x4 __attribute__((ext_vector_type(4)));
     typedef _Float16 x2 __attribute__((ext_vector_type(2)));
@@ -70,6 +83,15 @@ struct F16 {
         const x2 v = __builtin_bit_cast(x2, w);
         return pack((float)v[0] * f, (float)v[1] * f);
     }
+};
+
+// The same over a pool of 8-bit codes (e4m3) with a power-of-two scale per block: Q, the weights and the
+// output are E's, K and V are widened to E on their way into the matrix unit.  Widening is exact: a code has 4
+// significant bits, and its scale only moves the exponent (half precision: as far as it reaches down to 2^-24; the
+// append keeps values that would round up to 2^16 out).
+template <class E> struct Kv8 : E {
+    typedef E Wide;
+    static constexpr bool kEightBit = true;
 };
 
 }  // namespace cs

@@ -15,14 +15,15 @@
 // chosen by the host: 1 or 2 beside the tiles, 1 behind them when the decode side is the small one.
 #include "cs_prefill_impl.h"
 #include "cs_decode_impl.h"
+#include "cs_decode8_impl.h"
 
 namespace cs {
 
 static_assert(kPrefillThreads == kDecodeThreads, "one block size for both kinds of workgroup");
 
-template <int D>
+template <int D, bool kEightBit>
 union MixedLds {
-    PrefillLds<D> prefill;
+    PrefillLds<D, kEightBit> prefill;
     DecodeLds<D> decode;
 };
 
@@ -45,7 +46,7 @@ __global__ __launch_bounds__(kPrefillThreads, 2) void mixed_kernel(
     const ItemsInArgs items, const DecodePartials part, uint64_t tiles_launch,
     int32_t layers, int64_t next_layer, int64_t next_q)
 {
-    __shared__ MixedLds<D> lds;
+    __shared__ MixedLds<D, E::kEightBit> lds;
     if (blockIdx.x < dec_first || blockIdx.x >= dec_first + dec_wgs) {
         uint32_t ti = blockIdx.x < dec_first ? blockIdx.x : blockIdx.x - dec_wgs;
         const uint32_t wgs_whole = (uint32_t)cut_first_pos * Hkv, wgs_per_range = (uint32_t)(num_slots - cut_first_pos) * Hkv;
@@ -89,7 +90,12 @@ __global__ __launch_bounds__(kPrefillThreads, 2) void mixed_kernel(
             // one page ahead, with loads the compiler can count (a workgroup that shares its CU
             // with a tile must stream by itself); a deeper queue only delays the tile's own
             // copies, which share the CU's memory pipeline
-            decode_item<D, ItemsInArgs, E, 1, PS, Loads::kCounted>(lds.decode, layer_base + l * next_layer, page_stride, num_pages, Hkv, G, block_tables,
+            if constexpr (E::kEightBit)
+                decode_item8<D, ItemsInArgs, E, 1, Loads::kCounted>(lds.decode, layer_base + l * next_layer, page_stride, num_pages, Hkv, G, block_tables,
+                                           max_blocks, items, ctx_lens, cu_q_lens, q + l * next_q, out + l * next_q, scale_log2e,
+                                           mine, item, g);
+            else
+                decode_item<D, ItemsInArgs, E, 1, PS, Loads::kCounted>(lds.decode, layer_base + l * next_layer, page_stride, num_pages, Hkv, G, block_tables,
                                            max_blocks, items, ctx_lens, cu_q_lens, q + l * next_q, out + l * next_q, scale_log2e,
                                            mine, item, g);
             // (in place only where every workgroup has one pair)
@@ -104,6 +110,7 @@ static int launch_mixed_as(const cs_kv_pool& pool, int32_t layer, const LayerSpa
                            const PrefillPlan& pplan, const void* q, void* out, int32_t Hq, float scale,
                            void* decode_ws, void* prefill_ws, hipStream_t st, int32_t prio, int32_t persistent_wgs)
 {
+    constexpr int kOtherPage = E::kEightBit ? 16 : 8;                  // (8-bit pools have pages of 16 only)
     const int32_t Hkv = pool.num_kv_heads, D = pool.head_dim, G = Hq / Hkv;
     const uint16_t* layer_base = (const uint16_t*)pool.base + (int64_t)layer * pool.layer_stride;
     const float scale_log2e = scale * 1.4426950408889634f;
@@ -125,7 +132,7 @@ static int launch_mixed_as(const cs_kv_pool& pool, int32_t layer, const LayerSpa
                        (float*)prefill_ws, (uint32_t)dec_first, (uint32_t)dec_wgs, (uint32_t)n_decode, (int32_t)pplan.backwards,    \
                        dplan.arg_items, part, pplan.merges_in_place ? part.launch : 0, span.n, span.pool, span.q);
 #define CS_LAUNCH_MIXED(DD, PRIO)                                                                            \
-    if (pool.page_size == 16) { CS_LAUNCH_MIXED_P(DD, PRIO, 16) } else { CS_LAUNCH_MIXED_P(DD, PRIO, 8) }
+    if (pool.page_size == 16) { CS_LAUNCH_MIXED_P(DD, PRIO, 16) } else { CS_LAUNCH_MIXED_P(DD, PRIO, kOtherPage) }
     if (D == 128) { if (prio == 2) { CS_LAUNCH_MIXED(128, 2) } else if (prio == 1) { CS_LAUNCH_MIXED(128, 1) } else { CS_LAUNCH_MIXED(128, 0) } }
     else          { if (prio == 2) { CS_LAUNCH_MIXED(64, 2) } else if (prio == 1) { CS_LAUNCH_MIXED(64, 1) } else { CS_LAUNCH_MIXED(64, 0) } }
 #undef CS_LAUNCH_MIXED
@@ -147,6 +154,15 @@ int launch_mixed(const cs_kv_pool& pool, int32_t layer, const cs_batch& b, const
 {
     return launch_mixed_layers(pool, layer, LayerSpan{1, 0, 0, 0}, b, dplan, pplan, q, out, Hq, scale, decode_ws, prefill_ws, st, f16,
                                prio, persistent_wgs);
+}
+
+int launch_mixed_kv8(const cs_kv_pool& pool, int32_t layer, const cs_batch& b, const DecodePlan& dplan, const PrefillPlan& pplan,
+                     const void* q, void* out, int32_t Hq, float scale, void* decode_ws, void* prefill_ws, hipStream_t st, bool f16,
+                     int32_t prio, int32_t persistent_wgs)
+{
+    const LayerSpan one = {1, 0, 0, 0};
+    return f16 ? launch_mixed_as<Kv8<F16>>(pool, layer, one, b, dplan, pplan, q, out, Hq, scale, decode_ws, prefill_ws, st, prio, persistent_wgs)
+               : launch_mixed_as<Kv8<Bf16>>(pool, layer, one, b, dplan, pplan, q, out, Hq, scale, decode_ws, prefill_ws, st, prio, persistent_wgs);
 }
 
 }  // namespace cs

@@ -25,7 +25,8 @@ struct Plans {
 // The plan of a batch for launches of `layers` layers each (remembered per thread; the reference is
 // good until the thread asks for six more).  Sequences and tiles are cut as for one layer, whatever
 // `layers` is: how many layers share a launch changes no bit of their results.
-const Plans& plans_for(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D, int32_t layers = 1);
+// elem_bytes: of K and V (1: an 8-bit pool).
+const Plans& plans_for(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D, int32_t layers = 1, int32_t elem_bytes = 2);
 
 // The workspace a launch of `layers` layers may need: at least plans_for(..., layers).need, without making
 // that plan; nothing where one layer needs nothing.

@@ -16,7 +16,7 @@ __global__ __launch_bounds__(kPrefillThreads, 2) void prefill_kernel(
     int32_t range_steps, int32_t base_slot, float* __restrict__ part, int32_t n_ordered, const SlotOrder order,
     int32_t backwards, int64_t next_layer, int64_t next_q, int64_t next_part)
 {
-    __shared__ PrefillLds<D> lds;
+    __shared__ PrefillLds<D, E::kEightBit> lds;
     const int32_t pos = blockIdx.x / Hkv;
     const int32_t g = blockIdx.x - pos * Hkv;
     const int32_t b = n_ordered > 0 ? (int32_t)order.slot[pos]
@@ -154,6 +154,7 @@ template <class E>
 static int launch_prefill_as(const cs_kv_pool& pool, int32_t layer, const LayerSpan& span, const cs_batch& b, const PrefillPlan& plan,
                              const void* q, void* out, int32_t Hq, float scale, void* workspace, hipStream_t st)
 {
+    constexpr int kOtherPage = E::kEightBit ? 16 : 8;                  // (8-bit pools have pages of 16 only)
     const int32_t Hkv = pool.num_kv_heads, D = pool.head_dim, G = Hq / Hkv;
     const uint16_t* layer_base = (const uint16_t*)pool.base + (int64_t)layer * pool.layer_stride;
     const float scale_log2e = scale * 1.4426950408889634f;
@@ -169,9 +170,9 @@ static int launch_prefill_as(const cs_kv_pool& pool, int32_t layer, const LayerS
                        plan.range_steps, plan.base_slot, part, plan.n_ordered, plan.order, (int32_t)plan.backwards, \
                        span.pool, span.q, next_part);
     if (pool.page_size == 16) { if (D == 128) { CS_LAUNCH_PREFILL(128, 16) } else { CS_LAUNCH_PREFILL(64, 16) } }
-    else                      { if (D == 128) { CS_LAUNCH_PREFILL(128, 8) } else { CS_LAUNCH_PREFILL(64, 8) } }
+    else                      { if (D == 128) { CS_LAUNCH_PREFILL(128, kOtherPage) } else { CS_LAUNCH_PREFILL(64, kOtherPage) } }
 #undef CS_LAUNCH_PREFILL
-    if (plan.max_ranges > 1) launch_merge_as<E>(pool, span, b, plan, out, Hq, workspace, st);
+    if (plan.max_ranges > 1) launch_merge_as<typename E::Wide>(pool, span, b, plan, out, Hq, workspace, st);
     return check_launch("prefill kernels");
 }
 
@@ -194,6 +195,14 @@ int launch_prefill(const cs_kv_pool& pool, int32_t layer, const cs_batch& b, con
                    const void* q, void* out, int32_t Hq, float scale, void* workspace, hipStream_t st, bool f16)
 {
     return launch_prefill_layers(pool, layer, LayerSpan{1, 0, 0, 0}, b, plan, q, out, Hq, scale, workspace, st, f16);
+}
+
+int launch_prefill_kv8(const cs_kv_pool& pool, int32_t layer, const cs_batch& b, const PrefillPlan& plan, const void* q, void* out,
+                       int32_t Hq, float scale, void* workspace, hipStream_t st, bool f16)
+{
+    const LayerSpan one = {1, 0, 0, 0};
+    return f16 ? launch_prefill_as<Kv8<F16>>(pool, layer, one, b, plan, q, out, Hq, scale, workspace, st)
+               : launch_prefill_as<Kv8<Bf16>>(pool, layer, one, b, plan, q, out, Hq, scale, workspace, st);
 }
 
 }  // namespace cs

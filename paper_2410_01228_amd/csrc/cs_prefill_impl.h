@@ -116,10 +116,12 @@ __device__ __forceinline__ float* partials_of(float* part, int32_t cut_pos, int3
     return part + ((int64_t)cut_pos * Hkv + g) * max_ranges * kPartialFloats<D>;
 }
 
-// LDS of one prefill workgroup: the ring of K and of V steps.
-template <int D>
+// LDS of one prefill workgroup: the ring of K and of V steps.  From an 8-bit pool a step is written once its codes
+// are in registers, so the K of one step and the V of three are all that wait in LDS.
+constexpr int kRing8K = 2;
+template <int D, bool kEightBit = false>
 struct PrefillLds {
-    u32x4 k[kRing][4 * D];                            // 2 pages x 2*D 16-byte units per step
+    u32x4 k[kEightBit ? kRing8K : kRing][4 * D];      // 2 pages x 2*D 16-byte units per step
     u32x4 v[kRing][4 * D];
     int32_t last;                                     // all other ranges of this workgroup's cut tile are done
 };
@@ -138,7 +140,7 @@ struct PrefillLds {
 // partials to prefill_merge_kernel.
 template <int D, class E, int kPriority, int PS, bool kLaneAddr16, bool kMergeInGrid>
 __device__ __forceinline__ void prefill_tile(
-    PrefillLds<D>& lds,
+    PrefillLds<D, E::kEightBit>& lds,
     const uint16_t* __restrict__ layer_base, int64_t page_stride, int32_t num_pages,
     int32_t Hkv, int32_t G, int32_t S,
     const int32_t* __restrict__ block_tables, int32_t max_blocks,
@@ -162,6 +164,9 @@ __device__ __forceinline__ void prefill_tile(
     constexpr bool kLaneAddr = PS == 8 || kLaneAddr16;
     constexpr int kStepLoads = (kLaneAddr ? 2 : 2 * kStepPages) * kLoads;   // LDS-DMA instructions per wavefront and step
     constexpr int kPartRow = D + 4;                   // floats per query row of a partial: D outputs, max, sum, pad
+    constexpr bool kEight = E::kEightBit;
+    constexpr int kSlotsK = kEight ? kRing8K : kRing;
+    static_assert(!kEight || PS == 16, "8-bit pools have pages of 16 tokens");
     auto& lds_k = lds.k;
     auto& lds_v = lds.v;
 
@@ -271,7 +276,7 @@ __device__ __forceinline__ void prefill_tile(
     auto load_window = [&]() {
         const int32_t id = idbase + lane < n_pages ? table[idbase + lane] : 0;
         const uint64_t off = ((uint64_t)((id < 0 || id >= num_pages) ? 0 : id) * (uint64_t)page_stride
-                              + (uint64_t)g * (PS * D)) * 2;
+                              + (uint64_t)g * (kEight ? PS * D / 2 : PS * D)) * 2;
         pgoff_lo = (uint32_t)off;
         pgoff_hi = (uint32_t)(off >> 32);
         asm volatile("" : "+v"(pgoff_lo), "+v"(pgoff_hi));   // take the load's wait here, not at every readlane
@@ -337,6 +342,63 @@ __device__ __forceinline__ void prefill_tile(
         }
     };
 
+    // ---- 8-bit pools: a step's codes come into registers an iteration before they are needed, one 16-byte unit of
+    // K and one of V a lane (head dim 64: of K in the lower two wavefronts, of V in the upper two), are widened there,
+    // once a workgroup, and written to LDS in the arrangement above.  A K unit is 16 features of a token, two units of
+    // the step; a V unit 4 tokens of a feature in each of 4 feature tiles, half a unit of the step in each.  (Widened by every
+    // wavefront as it reads its operands, a step would cost each four times the conversions: 64 of them beside 34 matrix
+    // instructions.) ----
+    constexpr int kUnits8 = D / 64;
+    struct Codes { u32x4 u[kUnits8]; float scale[kUnits8]; };
+    const bool k_wave = D == 128 || wave < 2, v_wave = D == 128 || wave >= 2;
+    const int k_row = lane & 15, k_tile = (lane >> 4) & 1, k_half = lane >> 5;         // the 8 rows of a page are consecutive lanes: writes without bank conflicts
+    const int v_page = wave & 1, v_dtq = D == 128 ? wave >> 1 : 0, v_tg = lane >> 4;
+    const uint32_t k_off8 = (uint32_t)((((wave & (D / 32 - 1)) * 2 + k_half) * 16 + ((k_row >> 2) & 1) * 8 + (k_row & 3) + 4 * k_tile) * 16);
+    const uint32_t v_off8 = (uint32_t)(Hkv * (PS * D) + ((v_dtq * 4 + v_tg) * 16 + (lane & 15)) * 16);
+    const uint32_t s_off8 = (uint32_t)((2 * Hkv - g) * (PS * D) + g * 4);              // from a page's K block to its K scale
+    auto window8 = [&](int32_t step) {                    // in front of fetch8(step): a branch, out of the way of its scheduling
+        if (kStepPages * step - idbase >= 64) {          // steps only ever grow
+            idbase += 64;
+            load_window();
+        }
+    };
+    auto fetch8 = [&](int32_t step) -> Codes {
+        const int j = kStepPages * step - idbase;
+        Codes c;
+        auto unit = [&](int u, int page, uint32_t off, uint32_t scale_off) {
+            const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute((j + page) << 2, (int)pgoff_hi);
+            const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute((j + page) << 2, (int)pgoff_lo);
+            // (the lane's offset added with its carry: as a 64-bit sum it would take a register for its upper half, zero)
+            const uint32_t at = lo + off, carry = at < lo ? 1 : 0;
+            c.u[u] = *(const u32x4*)((const char*)layer_base + ((uint64_t)(hi + carry) << 32 | at));
+            c.scale[u] = *(const float*)((const char*)layer_base + scale_off + ((uint64_t)hi << 32 | lo));
+        };
+        if constexpr (D == 128) {
+            unit(0, k_row >> 3, k_off8, s_off8);
+            unit(kUnits8 - 1, v_page, v_off8, s_off8 + Hkv * 4);
+        } else {
+            unit(0, k_wave ? k_row >> 3 : v_page, k_wave ? k_off8 : v_off8, s_off8 + (k_wave ? 0 : Hkv * 4));
+        }
+        return c;
+    };
+    auto store8 = [&](int32_t step, const Codes& c) {
+        if (k_wave) {
+            const u32x4 w = c.u[0];
+            const float f = c.scale[0];
+            u32x4* to = &lds_k[(uint32_t)step % kSlotsK][(((wave & (D / 32 - 1)) * 2 + k_tile) * 4 + 2 * k_half) * 16 + k_row];
+            to[0] = u32x4{E::template widen<false>(w[0], f), E::template widen<true>(w[0], f), E::template widen<false>(w[1], f), E::template widen<true>(w[1], f)};
+            to[16] = u32x4{E::template widen<false>(w[2], f), E::template widen<true>(w[2], f), E::template widen<false>(w[3], f), E::template widen<true>(w[3], f)};
+        }
+        if (v_wave) {
+            const u32x4 w = c.u[kUnits8 - 1];
+            const float f = c.scale[kUnits8 - 1];
+            u32x2* to = (u32x2*)&lds_v[(uint32_t)step % kRing][v_dtq * 256 + (v_page * 2 + (v_tg >> 1)) * 16 + (lane & 15)] + (v_tg & 1);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                to[e * 128] = u32x2{E::template widen<false>(w[e], f), E::template widen<true>(w[e], f)};
+        }
+    };
+
     // Raw scores of one step (before the softmax scale).  With hi = lane/16: xs[c][0..3] are
     // rows 4*hi + i of tile X, xs[c][4..7] of tile Y, i.e. together the 8 consecutive keys
     // 32*step + 16*(hi/2) + 8*(hi%2) + 0..7.  Masked entries become -inf.
@@ -350,7 +412,7 @@ __device__ __forceinline__ void prefill_tile(
     for (int c = 0; c < kNCT; ++c) neg_off[c] = f32x4{0.f, 0.f, 0.f, 0.f};
     u32x4 kreg[2 * (D / 32)];
     auto load_k = [&](int32_t step) {
-        const u32x4* kA = &lds_k[(uint32_t)step % kRing][0];
+        const u32x4* kA = &lds_k[(uint32_t)step % kSlotsK][0];
 #pragma unroll
         for (int u = 0; u < 2 * (D / 32); ++u) kreg[u] = kA[u * 64 + lane];   // (kk*2 + tile)
     };
@@ -436,15 +498,38 @@ __device__ __forceinline__ void prefill_tile(
 
     // ---- prologue: the first kRing-1 steps of the range in flight, the first two landed,
     // scores of the first step, K operands of the second ----
+    StepPages pg_next;                                            // pages of the step issued next
+    Codes codes;                                                  // 8-bit: the codes of the step stored next
+    if constexpr (kEight) {
+        {
+            codes = fetch8(step_begin);
+            window8(step_begin + 1);
+            const Codes second = fetch8(step_begin + 1);
+            store8(step_begin, codes);
+            window8(step_begin + 2);
+            codes = fetch8(step_begin + 2);
+            store8(step_begin + 1, second);
+        }
+        __syncthreads();
+        load_k(step_begin);
+        scores(std::true_type{}, step_begin, x);
+        raise_max(x);
+        load_k(step_begin + 1);
+        __syncthreads();                                          // every wavefront has read the slot of the first step's K
+        store8(step_begin + 2, codes);
+        window8(step_begin + 3);
+        codes = fetch8(step_begin + 3);
+    } else {
 #pragma unroll
-    for (int j = 0; j < kRing - 1; ++j) dma_step(step_begin + j, step_pages(step_begin + j));
-    StepPages pg_next = step_pages(step_begin + kRing - 1);       // pages of the step issued next
-    wait_vmcnt<(kRing - 3) * kStepLoads>();
-    __syncthreads();
-    load_k(step_begin);
-    scores(std::true_type{}, step_begin, x);
-    raise_max(x);
-    load_k(step_begin + 1);
+        for (int j = 0; j < kRing - 1; ++j) dma_step(step_begin + j, step_pages(step_begin + j));
+        pg_next = step_pages(step_begin + kRing - 1);
+        wait_vmcnt<(kRing - 3) * kStepLoads>();
+        __syncthreads();
+        load_k(step_begin);
+        scores(std::true_type{}, step_begin, x);
+        raise_max(x);
+        load_k(step_begin + 1);
+    }
 
     // ---- iteration i.  First half: scores of step i+1 (into xn, from the K operands already in
     // registers) side by side with the weights of step i (from xc); the V operands of step i
@@ -453,6 +538,8 @@ __device__ __forceinline__ void prefill_tile(
     // i+2 are fetched and the new scores are tested against the running maxima.
     // kMask: causal / end-of-sequence masking (needed from the first edge step on);
     // kLast: there is no step i+1. ----
+    // From an 8-bit pool, the second half of iteration i also widens the codes of step i+3 (in the registers `codes`) into the
+    // slots that K(i+1) and V(i-1) left before the barrier, and sends for those of step i+4.
     auto iteration = [&](auto masked, auto last, int32_t i, float (&xc)[kNCT][8], float (&xn)[kNCT][8]) {
         constexpr bool kMask = decltype(masked)::value;
         constexpr bool kLast = decltype(last)::value;
@@ -463,8 +550,12 @@ __device__ __forceinline__ void prefill_tile(
         // half gets the matrix pipe whenever it asks, the exp / convert work of the other fills
         // the issue slots in between (measured: 7-9% on every shape).
         if (kPriority) __builtin_amdgcn_s_setprio(kPriority - 1);
-        dma_step(i + kRing - 1, pg_next);
-        pg_next = step_pages(i + kRing);               // consumed by the next iteration
+        if constexpr (!kEight) {
+            dma_step(i + kRing - 1, pg_next);
+            pg_next = step_pages(i + kRing);           // consumed by the next iteration
+        } else if (!kLast) {
+            window8(i + 4);
+        }
 
         if (!kLast) scores(masked, i + 1, xn);
         u32x4 pb[kNCT];
@@ -494,6 +585,45 @@ __device__ __forceinline__ void prefill_tile(
             av[dt] = vA[dt * 64 + lane];
             if (kMask) { av[dt][0] &= vm[0]; av[dt][1] &= vm[1]; av[dt][2] &= vm[2]; av[dt][3] &= vm[3]; }
         }
+        if constexpr (kEight && kMask) {
+            // A V that is not a number must stay with the rows that see its token: a weight of zero would spread it.  Such values
+            // are replaced by zeros here, and put into the outputs of the rows that see one, feature by feature, by
+            // one more product of ones: where a NaN is, by where the mask lets the row look.  (Edge steps only: the
+            // others hide no key from a row.)
+            auto nans = [](uint32_t w) {                              // bit 15 of each half that is none
+                return ((w & 0x7fff7fffu) + (0x7fffu - E::kInfinity) * 0x00010001u) & 0x80008000u;
+            };
+            uint32_t any = 0;
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any |= nans(av[dt][e]);
+            if (__any(any != 0)) {
+                const int32_t key0 = i * kKeysPerStep + (lane >> 5) * 16 + ((lane >> 4) & 1) * 8;
+                u32x4 sees[kNCT];
+#pragma unroll
+                for (int c = 0; c < kNCT; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        sees[c][e] = (key0 + 2 * e <= pos_q[c] ? E::kOnes & 0xffffu : 0u) | (key0 + 2 * e + 1 <= pos_q[c] ? E::kOnes & 0xffff0000u : 0u);
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) {
+                    u32x4 there;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t m = nans(av[dt][e]) >> 15;     // a one in each half
+                        there[e] = m * (E::kOnes & 0xffffu);
+                        av[dt][e] &= ~(m * 0xffffu);
+                    }
+#pragma unroll
+                    for (int c = 0; c < kNCT; ++c) {
+                        const f32x4 hit = E::mfma32(there, sees[c], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[c][dt][e] = hit[e] > 0.f ? __builtin_nanf("") : o[c][dt][e];
+                    }
+                }
+            }
+        }
         if (!kMask && !kLast) {
             // steady state, first half: tell the scheduler the order we want.  The exp / convert
             // work of step i runs under the score MFMAs of step i+1, and the V operands are
@@ -510,12 +640,16 @@ __device__ __forceinline__ void prefill_tile(
         // K(i+2) and V(i+1) must have landed before anyone reads them: all but the copies of
         // the last kRing-3 steps issued
         __builtin_amdgcn_sched_barrier(0);             // nothing may move across the two halves
-        wait_vmcnt<(kRing - 3) * kStepLoads>();
+        if constexpr (!kEight) wait_vmcnt<(kRing - 3) * kStepLoads>();
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
 
         if (kPriority) __builtin_amdgcn_s_setprio(kPriority);
         if (!kLast) load_k(i + 2);
+        if constexpr (kEight && !kLast) {
+            store8(i + 3, codes);
+            codes = fetch8(i + 4);
+        }
 #pragma unroll
         for (int c = 0; c < kNCT; ++c)
             lacc[c] = E::mfma32(ones, pb[c], lacc[c]);

@@ -1,0 +1,184 @@
+"""The 8-bit pool and the page calls without a GPU: the oracle against torch's conversions and a worked page, and what the
+calls refuse before anything would be enqueued."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv8
+from paper_2410_01228_amd import binding as cs
+
+
+def test_oracle_codes_are_e4m3():
+    codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy()
+    assert np.array_equal(np.isnan(codes), np.isnan(kv8.VALUES))
+    assert np.array_equal(codes[~np.isnan(codes)], kv8.VALUES[~np.isnan(codes)].astype(np.float32))
+    # every halfway point between neighbours, and either side of it
+    pos = kv8.VALUES[:127]
+    mid = (pos[1:] + pos[:-1]) / 2
+    x = np.concatenate([pos, mid, mid * (1 - 2.0 ** -20), mid * (1 + 2.0 ** -20)])
+    x = np.concatenate([x, -x]).astype(np.float32)
+    want = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    assert np.array_equal(kv8.encode(x), want)
+    assert kv8.encode(np.nan) & 127 == 127 and kv8.encode(1e9) == 126 and kv8.encode(-np.inf) == 254
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_oracle_places_fill_a_block_once(D):
+    t, d = np.arange(16)[:, None], np.arange(D)
+    for index in (kv8.k_index, kv8.v_index):
+        assert sorted(index(t, d).ravel()) == list(range(16 * D))
+    # a unit of K is 16 features of a token, a unit of V 4 tokens of a feature in 4 feature tiles
+    assert list(kv8.k_index(3, np.arange(16, 32))) == [(16 + 3) * 16 + i for i in range(16)]
+    assert list(kv8.v_index(np.arange(4, 8), 2)) == [(16 + 2) * 16 + i for i in range(4)]
+    assert kv8.v_index(4, 18) == (16 + 2) * 16 + 4
+
+
+@pytest.mark.parametrize("top,e", [(448.0, 0), (448.01, 1), (224.0, -1), (1.0, -8), (1.75, -8), (1.76, -7), (0.0, -100), (1e-35, -100)])
+def test_oracle_exponent(top, e):
+    assert kv8.exponent_for(top) == e
+
+
+def test_page_bytes():
+    assert cs.cs_kv8_page_bytes(8, 128) == 2 * 8 * 16 * 128 + 64 == kv8.page_bytes(8, 128)
+    assert cs.cs_kv8_page_bytes(1, 64) == 2 * 16 * 64 + 16 == kv8.page_bytes(1, 64)       # 8 bytes of scales, 8 of padding
+    assert cs.cs_kv8_page_bytes(3, 128) % 16 == 0
+    for bad in ((0, 128), (-1, 64), (8, 96), (8, 0), (70000, 128)):
+        assert cs.cs_kv8_page_bytes(*bad) == 0
+
+
+def _pool8(base=0x1000, L=2, P=8, Hkv=2, D=64, ps=None, ls=None):
+    ps = 2 * Hkv * (16 * D + 4) if ps is None else ps
+    return cs.cs_kv8_pool(base, L, P, Hkv, D, P * ps if ls is None else ls, ps)
+
+
+def _batch(ctx, ql, blocks=64, dev=0x2000):
+    h = torch.tensor(ctx, dtype=torch.int32)
+    cu = torch.zeros(len(ql) + 1, dtype=torch.int32)
+    cu[1:] = torch.cumsum(torch.tensor(ql, dtype=torch.int32), 0)
+    return cs.cs_batch(len(ctx), int(cu[-1]), dev, blocks, dev, dev, h.data_ptr(), cu.data_ptr()), (h, cu)
+
+
+BAD_POOLS = [
+    (dict(base=0), cs.CS_ERR_INVALID_ARG), (dict(base=0x1008), cs.CS_ERR_INVALID_ARG), (dict(L=0), cs.CS_ERR_INVALID_ARG),
+    (dict(P=0), cs.CS_ERR_INVALID_ARG), (dict(Hkv=0, ps=64), cs.CS_ERR_INVALID_ARG), (dict(D=96), cs.CS_ERR_UNSUPPORTED), (dict(D=256), cs.CS_ERR_UNSUPPORTED),
+    (dict(ps=2 * 2 * 16 * 64), cs.CS_ERR_INVALID_ARG), (dict(ps=4120), cs.CS_ERR_INVALID_ARG), (dict(ls=7 * 4128), cs.CS_ERR_INVALID_ARG),
+    (dict(ls=8 * 4128 + 8), cs.CS_ERR_INVALID_ARG), (dict(ps=1 << 62, ls=0), cs.CS_ERR_INVALID_ARG),
+]
+
+
+@pytest.mark.parametrize("change,status", BAD_POOLS)
+def test_pools_that_are_refused(change, status):
+    pool, (b, _keep) = _pool8(**change), _batch([3], [1])
+    L, P, B = cs.lib(), ctypes.byref, ctypes.byref
+    for f16 in ("", "_f16"):
+        assert getattr(L, "cs_kv8_append" + f16)(P(pool), 0, B(b), 0x3000, 0x4000, None) == status
+        assert getattr(L, "cs_paged_attention_mixed_kv8" + f16)(P(pool), 0, B(b), 0x3000, 0x4000, 4, 1.0, None, 0, None) == status
+    assert L.cs_kv8_page_space(P(pool), ctypes.byref(cs.cs_page_space())) == status
+
+
+def test_append_and_attention_refusals():
+    L, r = cs.lib(), ctypes.byref
+    pool, (b, _keep) = _pool8(), _batch([3, 0], [1, 20])
+    inv = cs.CS_ERR_INVALID_ARG
+    for fn in (L.cs_kv8_append, L.cs_kv8_append_f16):
+        assert fn(None, 0, r(b), 0x3000, 0x4000, None) == inv
+        assert fn(r(pool), -1, r(b), 0x3000, 0x4000, None) == inv and fn(r(pool), 2, r(b), 0x3000, 0x4000, None) == inv
+        assert fn(r(pool), 0, None, 0x3000, 0x4000, None) == inv
+        assert fn(r(pool), 0, r(b), None, 0x4000, None) == inv and fn(r(pool), 0, r(b), 0x3000, None, None) == inv
+        assert fn(r(pool), 0, r(b), 0x3008, 0x4000, None) == inv and fn(r(pool), 0, r(b), 0x3000, 0x4004, None) == inv
+        empty, (_k, _c) = _batch([], [])
+        assert fn(r(pool), 0, r(empty), None, None, None) == cs.CS_OK
+        short, _k2 = _batch([60], [10], blocks=4)
+        assert fn(r(pool), 0, r(short), 0x3000, 0x4000, None) == inv                       # the table is too narrow
+    for fn in (L.cs_paged_attention_mixed_kv8, L.cs_paged_attention_mixed_kv8_f16):
+        def call(p=pool, layer=0, batch=b, q=0x3000, out=0x4000, hq=4, scale=1.0, ws=None, n=0, fn=fn):
+            return fn(r(p), layer, r(batch), q, out, hq, scale, ws, n, None)
+        assert call(layer=2) == inv and call(hq=0) == inv and call(hq=3) == inv and call(hq=34) == cs.CS_ERR_UNSUPPORTED
+        assert call(q=None) == inv and call(out=0) == inv and call(q=0x3004) == inv and call(out=0x4008) == inv
+        for s in (0.0, -1.0, float("inf"), float("nan")):
+            assert call(scale=s) == inv
+        # a batch whose tiles or sequences are cut needs its workspace
+        cut, _k3 = _batch([100000], [1], blocks=8192)
+        need = L.cs_paged_attention_kv8_workspace_bytes(r(cut), 4, 2, 64)
+        assert need > 0
+        assert call(batch=cut) == inv and call(batch=cut, ws=0x5000, n=need - 1) == cs.CS_ERR_WORKSPACE_TOO_SMALL and call(batch=cut, ws=0x5008, n=need) == inv
+    assert L.cs_paged_attention_kv8_workspace_bytes(r(b), 4, 3, 64) == 0 and L.cs_paged_attention_kv8_workspace_bytes(None, 4, 2, 64) == 0
+
+
+def _space(base=0x1000, L=3, P=8, pb=4128, ls=None, ps=None):
+    ps = pb if ps is None else ps
+    return cs.cs_page_space(base, L, P, pb, P * ps if ls is None else ls, ps)
+
+
+def _tables(bt=0x2000, lens=0x3000, counts=0x4000, rows=4, blocks=8, pages=8, size=16):
+    return cs.cs_page_tables(bt, lens, counts, rows, blocks, pages, size)
+
+
+BAD_SPACES = [dict(base=0), dict(base=0x1004), dict(L=0), dict(P=0), dict(pb=0), dict(pb=4120), dict(ps=4112), dict(ps=4136), dict(ls=8 * 4128 - 16),
+              dict(ls=8 * 4128 + 4), dict(ps=(1 << 62) - 16)]
+BAD_TABLES = [dict(bt=0), dict(lens=0), dict(counts=0), dict(rows=0), dict(blocks=0), dict(pages=0), dict(size=0), dict(pages=9)]
+
+
+@pytest.mark.parametrize("change", BAD_SPACES)
+def test_page_spaces_that_are_refused(change):
+    L, r, inv = cs.lib(), ctypes.byref, cs.CS_ERR_INVALID_ARG
+    bad, good, t = _space(**change), _space(), _tables()
+    assert L.cs_kv_pages_copy(r(bad), 0, 0x5000, r(good), 0, 0x6000, 1, 2, None) == inv
+    assert L.cs_kv_pages_copy(r(good), 0, 0x5000, r(bad), 0, 0x6000, 1, 2, None) == inv
+    assert L.cs_kv_pages_fork(r(bad), 0, 1, r(t), 0x5000, 0x6000, 0x7000, 1, None) == inv
+    assert L.cs_kv_pages_compact(r(bad), 0, 1, r(t), r(t), 0x5000, 0x6000, 0x7000, 1 << 20, None) == inv
+
+
+@pytest.mark.parametrize("change", BAD_TABLES)
+def test_page_tables_that_are_refused(change):
+    L, r, inv = cs.lib(), ctypes.byref, cs.CS_ERR_INVALID_ARG
+    bad, s, t = _tables(**change), _space(), _tables()
+    assert L.cs_kv_pages_fork(r(s), 0, 1, r(bad), 0x5000, 0x6000, 0x7000, 1, None) == inv
+    assert L.cs_kv_pages_compact(r(s), 0, 1, r(bad), r(t), 0x5000, 0x6000, 0x7000, 1 << 20, None) == inv
+    assert L.cs_kv_pages_compact(r(s), 0, 1, r(t), r(bad), 0x5000, 0x6000, 0x7000, 1 << 20, None) == inv
+    if "pages" not in change or change["pages"] == 0:
+        assert L.cs_kv_pages_free(r(bad), 0x5000, 1, 0x6000, 0x7000, None) == inv
+
+
+def test_page_call_refusals():
+    L, r, inv = cs.lib(), ctypes.byref, cs.CS_ERR_INVALID_ARG
+    s, t = _space(), _tables()
+
+    def copy(src=s, sl=0, si=0x5000, dst=s, dl=0, di=0x6000, layers=1, n=2):
+        return L.cs_kv_pages_copy(r(src), sl, si, r(dst), dl, di, layers, n, None)
+    assert copy(n=0) == cs.CS_OK and copy(layers=0) == cs.CS_OK and copy(sl=3, layers=0) == cs.CS_OK
+    assert copy(n=-1) == inv and copy(layers=-1) == inv and copy(sl=-1) == inv and copy(dl=4, layers=0) == inv and copy(sl=2, layers=2) == inv
+    assert copy(dl=1, layers=3) == inv and copy(si=None, n=9) == inv and copy(di=None, n=9) == inv
+    assert copy(dst=_space(pb=4144)) == inv
+    fork = L.cs_kv_pages_fork
+    assert fork(r(s), 0, 1, r(t), None, None, None, 0, None) == cs.CS_OK
+    assert fork(r(s), 0, 1, r(t), 0x5000, 0x6000, 0x7000, -1, None) == inv
+    assert fork(r(s), 2, 1, r(t), 0x5000, 0x6000, 0x7000, 1, None) == inv and fork(r(s), 0, 4, r(t), 0x5000, 0x6000, 0x7000, 1, None) == inv
+    for k in range(3):
+        lists = [0x5000, 0x6000, 0x7000]
+        lists[k] = None
+        assert fork(r(s), 0, 1, r(t), *lists, 1, None) == inv
+    assert L.cs_kv_pages_free(r(t), None, 1, 0x6000, 0x7000, None) == inv and L.cs_kv_pages_free(r(t), 0x5000, -1, 0x6000, 0x7000, None) == inv
+    assert L.cs_kv_pages_free(r(t), 0x5000, 1, None, 0x7000, None) == inv and L.cs_kv_pages_free(r(t), 0x5000, 1, 0x6000, None, None) == inv
+    need = L.cs_kv_pages_compact_workspace_bytes(8)
+    assert need > 0 and L.cs_kv_pages_compact_workspace_bytes(0) == 0 == L.cs_kv_pages_compact_workspace_bytes(-5)
+
+    def compact(new=t, ids=0x5000, used=0x6000, ws=0x7000, n=need, l0=0, l1=3):
+        return L.cs_kv_pages_compact(r(s), l0, l1, r(t), r(new), ids, used, ws, n, None)
+    assert compact(ids=None) == inv and compact(used=None) == inv and compact(ws=None) == inv and compact(ws=0x7004) == inv
+    assert compact(n=need - 1) == cs.CS_ERR_WORKSPACE_TOO_SMALL and compact(l1=4) == inv and compact(l0=2, l1=1) == inv
+    assert compact(new=_tables(rows=5)) == inv and compact(new=_tables(blocks=7)) == inv and compact(new=_tables(size=8)) == inv
+
+
+def test_spaces_of_pools():
+    s = cs.cs_page_space()
+    p16 = cs.cs_kv_pool(0x1000, 2, 8, 16, 2, 64, 8 * 5000, 5000)
+    assert cs.lib().cs_kv_page_space(ctypes.byref(p16), ctypes.byref(s)) == cs.CS_OK
+    assert (s.base, s.num_layers, s.num_pages, s.page_bytes, s.layer_stride, s.page_stride) == (0x1000, 2, 8, 8192, 80000, 10000)
+    p8 = _pool8(ps=4224)
+    assert cs.lib().cs_kv8_page_space(ctypes.byref(p8), ctypes.byref(s)) == cs.CS_OK
+    assert (s.page_bytes, s.layer_stride, s.page_stride) == (4112, 8 * 4224, 4224)
+    assert cs.lib().cs_kv8_page_space(ctypes.byref(p8), None) == cs.CS_ERR_INVALID_ARG
+    assert cs.lib().cs_kv_page_space(ctypes.byref(p16), None) == cs.CS_ERR_INVALID_ARG
