@@ -21,9 +21,9 @@ namespace cs {
 
 static_assert(kPrefillThreads == kDecodeThreads, "one block size for both kinds of workgroup");
 
-template <int D, bool kEightBit>
+template <int D, int kCodes>
 union MixedLds {
-    PrefillLds<D, kEightBit> prefill;
+    PrefillLds<D, kCodes> prefill;
     DecodeLds<D> decode;
 };
 
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kPrefillThreads, 2) void mixed_kernel(
     const ItemsInArgs items, const DecodePartials part, uint64_t tiles_launch,
     int32_t layers, int64_t next_layer, int64_t next_q)
 {
-    __shared__ MixedLds<D, E::kEightBit> lds;
+    __shared__ MixedLds<D, E::kCodes> lds;
     if (blockIdx.x < dec_first || blockIdx.x >= dec_first + dec_wgs) {
         uint32_t ti = blockIdx.x < dec_first ? blockIdx.x : blockIdx.x - dec_wgs;
         const uint32_t wgs_whole = (uint32_t)cut_first_pos * Hkv, wgs_per_range = (uint32_t)(num_slots - cut_first_pos) * Hkv;

@@ -16,7 +16,7 @@ __global__ __launch_bounds__(kPrefillThreads, 2) void prefill_kernel(
     int32_t range_steps, int32_t base_slot, float* __restrict__ part, int32_t n_ordered, const SlotOrder order,
     int32_t backwards, int64_t next_layer, int64_t next_q, int64_t next_part)
 {
-    __shared__ PrefillLds<D, E::kEightBit> lds;
+    __shared__ PrefillLds<D, E::kCodes> lds;
     const int32_t pos = blockIdx.x / Hkv;
     const int32_t g = blockIdx.x - pos * Hkv;
     const int32_t b = n_ordered > 0 ? (int32_t)order.slot[pos]

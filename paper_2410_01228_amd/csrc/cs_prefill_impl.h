@@ -81,6 +81,15 @@ __device__ __forceinline__ void lds_dma16_two_pages(const void* base_a, const vo
                  : "s"(lds_addr), "v"(off), "s"(base_a), "s"(base_b), "s"(mask_a) : "memory", "m0", "scc");
 }
 
+// One LDS-DMA load from a scalar base and the lanes' 32-bit byte offsets.
+__device__ __forceinline__ void lds_dma16_one_page(const void* base, uint32_t off, void* dst_wave_base) {
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)dst_wave_base;
+    asm volatile("s_mov_b32 m0, %0\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, %2"
+                 :: "s"(lds_addr), "v"(off), "s"(base) : "memory", "m0");
+}
+
 // One LDS-DMA load whose lanes bring their own 64-bit global addresses (+ kImm bytes).  The
 // instruction's immediate offset moves BOTH ends of the copy -- the global address and the LDS
 // address (M0 + offset + lane*16) -- so M0 is set kImm short of the destination.  The s_nop
@@ -95,6 +104,15 @@ __device__ __forceinline__ void lds_dma16_lane_addr(uint64_t addr, void* dst_wav
                  :: "s"(lds_addr), "v"(addr), "n"(kImm) : "memory", "m0");
 }
 
+// The same, 4 bytes a lane, to LDS at base + lane*4.
+__device__ __forceinline__ void lds_dma4_lane_addr(uint64_t addr, void* dst_wave_base) {
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)dst_wave_base;
+    asm volatile("s_mov_b32 m0, %0\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dword %1, off"
+                 :: "s"(lds_addr), "v"(addr) : "memory", "m0");
+}
+
 // max(a, b, c) in one instruction.  fmaxf() makes the compiler canonicalise every operand
 // first (one extra v_max per value, to quiet signalling NaNs); the scores need no such care.
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -104,6 +122,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 __device__ __forceinline__ float max8(const float (&x)[8]) {
     return max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
+}
+// The same as instructions that the compiler knows (v_maximum3_f32; NaN if one of them is), so that it keeps them as far behind
+// the matrix instruction whose results they read as they have to be: no hardware waits for that.  An 8-bit product of
+// 128 values takes twice the passes of a 16-bit one of 32, and the asm above was put one instruction behind it: at head
+// dim 64 single rows read a maximum from before the product.
+__device__ __forceinline__ float maximum8(const float (&x)[8]) {
+    auto three = [](float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); };
+    return three(three(x[0], x[1], x[2]), three(x[3], x[4], x[5]), three(x[6], x[7], x[7]));
 }
 
 
@@ -116,15 +142,34 @@ __device__ __forceinline__ float* partials_of(float* part, int32_t cut_pos, int3
     return part + ((int64_t)cut_pos * Hkv + g) * max_ranges * kPartialFloats<D>;
 }
 
-// LDS of one prefill workgroup: the ring of K and of V steps.  From an 8-bit pool a step is written once its codes
-// are in registers, so the K of one step and the V of three are all that wait in LDS.
-constexpr int kRing8K = 2;
-template <int D, bool kEightBit = false>
+// LDS of one prefill workgroup: the ring of K and of V steps.
+template <int D, int kCodes = 0>
 struct PrefillLds {
-    u32x4 k[kEightBit ? kRing8K : kRing][4 * D];      // 2 pages x 2*D 16-byte units per step
+    u32x4 k[kRing][4 * D];                            // 2 pages x 2*D 16-byte units per step
     u32x4 v[kRing][4 * D];
     int32_t last;                                     // all other ranges of this workgroup's cut tile are done
 };
+// From an 8-bit pool: the codes of the next steps -- K as operands, V as the lanes' own 16-byte units, where they find them again
+// -- and the scales of 64 pages (two windows of them) for each wavefront; V once more, widened.
+constexpr int kAhead8 = 2;                            // steps on their way beyond the one that the next iteration needs
+constexpr int kRing8V = 2;
+// Three codes a value of Q are more registers than there are: the last ones wait in LDS (spilled by the compiler they come
+// back as memory loads, each of which waits for all copies under way: 1024 tokens on 30720 keys, 64/8 heads, 1020 us with them in
+// LDS, 1127 spilled; with those of one of the two column tiles in LDS the rest still spills, 1226).
+template <int D, int kCodes> constexpr bool kQInLds = kCodes == 3 && D == 128;
+template <int D>
+struct PrefillLds8 {
+    u32x4 k[kRing][2 * D];
+    u32x4 v_codes[kRing][2 * D];
+    u32x4 v[kRing8V][4 * D];
+    float scale[2][kPrefillWaves][2][64];             // [window][wavefront][K, V][page]
+    int32_t last;
+};
+template <int D> struct PrefillLds<D, 2> : PrefillLds8<D> {};
+template <int D> struct PrefillLds<D, 3> : PrefillLds8<D> {
+    u32x4 q_low[kQInLds<D, 3> ? kPrefillWaves : 1][kNCT][2][64];
+};
+static_assert(kAhead8 + 2 <= kRing, "K of the steps i+1 .. i+2+kAhead8");
 
 // The work of one prefill workgroup: the tile in slot b, kv head g, key range `range` (a tile
 // whose keys need more than range_steps steps is cut into ranges, each leaving a partial in
@@ -140,7 +185,7 @@ struct PrefillLds {
 // partials to prefill_merge_kernel.
 template <int D, class E, int kPriority, int PS, bool kLaneAddr16, bool kMergeInGrid>
 __device__ __forceinline__ void prefill_tile(
-    PrefillLds<D, E::kEightBit>& lds,
+    PrefillLds<D, E::kCodes>& lds,
     const uint16_t* __restrict__ layer_base, int64_t page_stride, int32_t num_pages,
     int32_t Hkv, int32_t G, int32_t S,
     const int32_t* __restrict__ block_tables, int32_t max_blocks,
@@ -165,7 +210,7 @@ __device__ __forceinline__ void prefill_tile(
     constexpr int kStepLoads = (kLaneAddr ? 2 : 2 * kStepPages) * kLoads;   // LDS-DMA instructions per wavefront and step
     constexpr int kPartRow = D + 4;                   // floats per query row of a partial: D outputs, max, sum, pad
     constexpr bool kEight = E::kEightBit;
-    constexpr int kSlotsK = kEight ? kRing8K : kRing;
+    constexpr int kSlotsV = kEight ? kRing8V : kRing;
     static_assert(!kEight || PS == 16, "8-bit pools have pages of 16 tokens");
     auto& lds_k = lds.k;
     auto& lds_v = lds.v;
@@ -199,9 +244,11 @@ __device__ __forceinline__ void prefill_tile(
     // kFold (element types that stand it, see cs_elem.h): Q is scaled once by scale*log2(e), so the
     // matrix unit delivers the scores in the exponent's domain, and the score accumulators start
     // from minus the running offset, so exp2 takes them as they come -- no multiply-add per score.
-    constexpr bool kFold = E::kScaleFoldsIntoQ;
+    // (not with 8-bit codes: three of them hold a half exactly, and the accumulators' start takes registers that are short)
+    constexpr bool kFold = E::kScaleFoldsIntoQ && !kEight;
     // ---- this wavefront's column tiles: ct = wave*4 + c -> (token block, head) ----
-    u32x4 qb[kNCT][D / 32];
+    u32x4 qb[kEight ? 1 : kNCT][D / 32];
+    QCodes<D, E> q8[kEight ? kNCT : 1];                // 8-bit pools: Q in codes too
     int32_t pos_q[kNCT];                               // absolute position of this lane's query
     const u32x4 zero4 = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -211,16 +258,24 @@ __device__ __forceinline__ void prefill_tile(
         const int32_t tl = tb * 16 + (lane & 15);            // chunk-local token of this column
         const bool valid = ct < n_ct && tl < q_len;
         pos_q[c] = C + tl;
+        if constexpr (kEight) {
+            q8[c].load(q + ((int64_t)(t_seq + tl) * Hq + g * G + hh) * D, valid, lane);
+            if constexpr (kQInLds<D, E::kCodes>) {
 #pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) {
-            u32x4 v = zero4;
-            if (valid)
-                v = *(const u32x4*)(q + ((int64_t)(t_seq + tl) * Hq + g * G + hh) * D + kk * 32 + (lane >> 4) * 8);
-            if constexpr (kFold) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = E::scale2(v[e], scale_log2e);
+                for (int u = 0; u < 2; ++u) lds.q_low[wave][c][u][lane] = q8[c].w[2][u];
             }
-            qb[c][kk] = v;
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk) {
+                u32x4 v = zero4;
+                if (valid)
+                    v = *(const u32x4*)(q + ((int64_t)(t_seq + tl) * Hq + g * G + hh) * D + kk * 32 + (lane >> 4) * 8);
+                if constexpr (kFold) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = E::scale2(v[e], scale_log2e);
+                }
+                qb[c][kk] = v;
+            }
         }
     }
 
@@ -273,6 +328,7 @@ __device__ __forceinline__ void prefill_tile(
     // steps; a page the sequence does not have (or a bad id) reads as page 0.
     int32_t idbase = (kStepPages * step_begin) & ~63;
     uint32_t pgoff_lo, pgoff_hi;
+    const uint32_t s_off8 = (uint32_t)((2 * Hkv - g) * (PS * D) + g * 4);              // from a page's K block to its K scale (8-bit)
     auto load_window = [&]() {
         const int32_t id = idbase + lane < n_pages ? table[idbase + lane] : 0;
         const uint64_t off = ((uint64_t)((id < 0 || id >= num_pages) ? 0 : id) * (uint64_t)page_stride
@@ -280,6 +336,11 @@ __device__ __forceinline__ void prefill_tile(
         pgoff_lo = (uint32_t)off;
         pgoff_hi = (uint32_t)(off >> 32);
         asm volatile("" : "+v"(pgoff_lo), "+v"(pgoff_hi));   // take the load's wait here, not at every readlane
+        if constexpr (kEight) {
+            const uint64_t at = (uint64_t)(uintptr_t)layer_base + off + s_off8;
+            lds_dma4_lane_addr(at, lds.scale[(idbase >> 6) & 1][wave][0]);
+            lds_dma4_lane_addr(at + Hkv * 4, lds.scale[(idbase >> 6) & 1][wave][1]);
+        }
     };
     load_window();
     // lane mode: which of the step's pages this lane's K units and V units come from
@@ -342,60 +403,66 @@ __device__ __forceinline__ void prefill_tile(
         }
     };
 
-    // ---- 8-bit pools: a step's codes come into registers an iteration before they are needed, one 16-byte unit of
-    // K and one of V a lane (head dim 64: of K in the lower two wavefronts, of V in the upper two), are widened there,
-    // once a workgroup, and written to LDS in the arrangement above.  A K unit is 16 features of a token, two units of
-    // the step; a V unit 4 tokens of a feature in each of 4 feature tiles, half a unit of the step in each.  (Widened by every
-    // wavefront as it reads its operands, a step would cost each four times the conversions: 64 of them beside 34 matrix
-    // instructions.) ----
-    constexpr int kUnits8 = D / 64;
-    struct Codes { u32x4 u[kUnits8]; float scale[kUnits8]; };
+    // ---- 8-bit pools.  K is never widened: its codes are copied to LDS as operands of the 8-bit matrix instruction (one 16-byte
+    // unit, 16 features of a token, is half a lane's operand), Q is split into codes (QCodes), and the instruction
+    // applies the blocks' scales.  V is copied as it is, a unit a lane; the lane that copied it reads it back an iteration later, widens
+    // it and writes it in the arrangement above -- once a workgroup, because widened by every wavefront as it reads
+    // its operands a step would cost each 32 conversions; the weights, unlike Q, are new every step, and splitting them would cost
+    // more than that.  A unit of V is 4 tokens of a feature in each of 4 feature tiles, half a 16-bit unit in each.
+    // Head dim 64: K is copied by the lower two wavefronts, V by the upper two. ----
+    constexpr int kLoads8 = D == 64 ? 1 : kLaneAddr ? 2 : 3;                           // LDS-DMA instructions per wavefront and step, at least
     const bool k_wave = D == 128 || wave < 2, v_wave = D == 128 || wave >= 2;
-    const int k_row = lane & 15, k_tile = (lane >> 4) & 1, k_half = lane >> 5;         // the 8 rows of a page are consecutive lanes: writes without bank conflicts
+    const int k_row = lane & 15, k_tile = wave & 1, k_u = D == 128 ? wave >> 1 : 0;
     const int v_page = wave & 1, v_dtq = D == 128 ? wave >> 1 : 0, v_tg = lane >> 4;
-    const uint32_t k_off8 = (uint32_t)((((wave & (D / 32 - 1)) * 2 + k_half) * 16 + ((k_row >> 2) & 1) * 8 + (k_row & 3) + 4 * k_tile) * 16);
+    const uint32_t k_off8 = (uint32_t)(((k_u * 4 + (lane >> 4)) * 16 + ((k_row >> 2) & 1) * 8 + (k_row & 3) + 4 * k_tile) * 16);
     const uint32_t v_off8 = (uint32_t)(Hkv * (PS * D) + ((v_dtq * 4 + v_tg) * 16 + (lane & 15)) * 16);
-    const uint32_t s_off8 = (uint32_t)((2 * Hkv - g) * (PS * D) + g * 4);              // from a page's K block to its K scale
-    auto window8 = [&](int32_t step) {                    // in front of fetch8(step): a branch, out of the way of its scheduling
-        if (kStepPages * step - idbase >= 64) {          // steps only ever grow
-            idbase += 64;
-            load_window();
+    const int unit0_8 = (D == 128 ? wave : wave & 1) * 64;
+    auto copy8 = [&](int32_t step) {
+        if constexpr (kEight) {
+            if (kStepPages * step - idbase >= 64) {          // steps only ever grow
+                idbase += 64;
+                load_window();
+            }
+            const int j = kStepPages * step - idbase;
+            u32x4* const k_to = &lds.k[(uint32_t)step % kRing][unit0_8];
+            u32x4* const v_to = &lds.v_codes[(uint32_t)step % kRing][unit0_8];
+            if constexpr (kLaneAddr) {
+                auto unit = [&](u32x4* dst, int page, uint32_t off) {
+                    const uint64_t o = ((uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute((j + page) << 2, (int)pgoff_hi) << 32)
+                                     | (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute((j + page) << 2, (int)pgoff_lo);
+                    lds_dma16_lane_addr<0>((uint64_t)(uintptr_t)layer_base + o + off, dst);
+                };
+                if constexpr (D == 128) {
+                    unit(k_to, k_row >> 3, k_off8);
+                    unit(v_to, v_page, v_off8);
+                } else {
+                    unit(k_wave ? k_to : v_to, k_wave ? k_row >> 3 : v_page, k_wave ? k_off8 : v_off8);
+                }
+            } else {
+                auto page = [&](int e) {
+                    const uint64_t o = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(pgoff_hi, j + e) << 32)
+                                     | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(pgoff_lo, j + e);
+                    return (const char*)layer_base + o;
+                };
+                if (k_wave) lds_dma16_two_pages(page(0), page(1), k_off8, 0x00ff00ff00ff00ffull, k_to);
+                if (v_wave) lds_dma16_one_page(page(v_page), v_off8, v_to);
+            }
         }
     };
-    auto fetch8 = [&](int32_t step) -> Codes {
-        const int j = kStepPages * step - idbase;
-        Codes c;
-        auto unit = [&](int u, int page, uint32_t off, uint32_t scale_off) {
-            const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_bpermute((j + page) << 2, (int)pgoff_hi);
-            const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute((j + page) << 2, (int)pgoff_lo);
-            // (the lane's offset added with its carry: as a 64-bit sum it would take a register for its upper half, zero)
-            const uint32_t at = lo + off, carry = at < lo ? 1 : 0;
-            c.u[u] = *(const u32x4*)((const char*)layer_base + ((uint64_t)(hi + carry) << 32 | at));
-            c.scale[u] = *(const float*)((const char*)layer_base + scale_off + ((uint64_t)hi << 32 | lo));
-        };
-        if constexpr (D == 128) {
-            unit(0, k_row >> 3, k_off8, s_off8);
-            unit(kUnits8 - 1, v_page, v_off8, s_off8 + Hkv * 4);
-        } else {
-            unit(0, k_wave ? k_row >> 3 : v_page, k_wave ? k_off8 : v_off8, s_off8 + (k_wave ? 0 : Hkv * 4));
-        }
-        return c;
+    auto scale8 = [&](int32_t step, int kv, int page) {
+        if constexpr (kEight) return lds.scale[(kStepPages * step >> 6) & 1][wave][kv][(kStepPages * step & 63) + page];
+        else return 0.f;
     };
-    auto store8 = [&](int32_t step, const Codes& c) {
-        if (k_wave) {
-            const u32x4 w = c.u[0];
-            const float f = c.scale[0];
-            u32x4* to = &lds_k[(uint32_t)step % kSlotsK][(((wave & (D / 32 - 1)) * 2 + k_tile) * 4 + 2 * k_half) * 16 + k_row];
-            to[0] = u32x4{E::template widen<false>(w[0], f), E::template widen<true>(w[0], f), E::template widen<false>(w[1], f), E::template widen<true>(w[1], f)};
-            to[16] = u32x4{E::template widen<false>(w[2], f), E::template widen<true>(w[2], f), E::template widen<false>(w[3], f), E::template widen<true>(w[3], f)};
-        }
-        if (v_wave) {
-            const u32x4 w = c.u[kUnits8 - 1];
-            const float f = c.scale[kUnits8 - 1];
-            u32x2* to = (u32x2*)&lds_v[(uint32_t)step % kRing][v_dtq * 256 + (v_page * 2 + (v_tg >> 1)) * 16 + (lane & 15)] + (v_tg & 1);
+    auto widen8 = [&](int32_t step) {
+        if constexpr (kEight) {
+            if (v_wave) {
+                const u32x4 w = lds.v_codes[(uint32_t)step % kRing][unit0_8 + lane];
+                const float f = scale8(step, 1, v_page);
+                u32x2* to = (u32x2*)&lds_v[(uint32_t)step % kSlotsV][v_dtq * 256 + (v_page * 2 + (v_tg >> 1)) * 16 + (lane & 15)] + (v_tg & 1);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                to[e * 128] = u32x2{E::template widen<false>(w[e], f), E::template widen<true>(w[e], f)};
+                for (int e = 0; e < 4; ++e)
+                    to[e * 128] = u32x2{E::template widen<false>(w[e], f), E::template widen<true>(w[e], f)};
+            }
         }
     };
 
@@ -410,11 +477,14 @@ __device__ __forceinline__ void prefill_tile(
     f32x4 neg_off[kNCT];
 #pragma unroll
     for (int c = 0; c < kNCT; ++c) neg_off[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    u32x4 kreg[2 * (D / 32)];
+    constexpr int kRegsK = kEight ? 2 * (D / 64) : 2 * (D / 32);
+    u32x4 kreg[kRegsK];
+    uint32_t k_scale = 0;                              // 8-bit: exponent of the block of this lane's row, in both tiles
     auto load_k = [&](int32_t step) {
-        const u32x4* kA = &lds_k[(uint32_t)step % kSlotsK][0];
+        const u32x4* kA = &lds_k[(uint32_t)step % kRing][0];
 #pragma unroll
-        for (int u = 0; u < 2 * (D / 32); ++u) kreg[u] = kA[u * 64 + lane];   // (kk*2 + tile)
+        for (int u = 0; u < kRegsK; ++u) kreg[u] = kA[u * 64 + lane];          // (kk*2 + tile)
+        if constexpr (kEight) k_scale = __builtin_bit_cast(uint32_t, scale8(step, 0, k_row >> 3)) >> 23;
     };
     auto scores = [&](auto masked, int32_t step, float (&xs)[kNCT][8]) {
         constexpr bool kMask = decltype(masked)::value;
@@ -424,12 +494,24 @@ __device__ __forceinline__ void prefill_tile(
             if constexpr (kFold) { s0[c] = neg_off[c]; s1[c] = neg_off[c]; }
             else { s0[c] = f32x4{0.f, 0.f, 0.f, 0.f}; s1[c] = f32x4{0.f, 0.f, 0.f, 0.f}; }
         }
-#pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) {
+        if constexpr (kEight) {
 #pragma unroll
             for (int c = 0; c < kNCT; ++c) {
-                s0[c] = E::mfma32(kreg[kk * 2 + 0], qb[c][kk], s0[c]);   // tile X
-                s1[c] = E::mfma32(kreg[kk * 2 + 1], qb[c][kk], s1[c]);   // tile Y
+                if constexpr (kQInLds<D, E::kCodes>) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) q8[c].w[2][u] = lds.q_low[wave][c][u][lane];
+                }
+                s0[c] = q8[c].dot(kreg[0], kreg[kRegsK - 2], k_scale, s0[c]);    // tile X
+                s1[c] = q8[c].dot(kreg[1], kreg[kRegsK - 1], k_scale, s1[c]);    // tile Y
+            }
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk) {
+#pragma unroll
+                for (int c = 0; c < kNCT; ++c) {
+                    s0[c] = E::mfma32(kreg[kk * 2 + 0], qb[c][kk], s0[c]);   // tile X
+                    s1[c] = E::mfma32(kreg[kk * 2 + 1], qb[c][kk], s1[c]);   // tile Y
+                }
             }
         }
         const int32_t key0 = step * kKeysPerStep + (lane >> 5) * 16 + ((lane >> 4) & 1) * 8;
@@ -458,12 +540,12 @@ __device__ __forceinline__ void prefill_tile(
         bool need = false;
 #pragma unroll
         for (int c = 0; c < kNCT; ++c) {
-            need |= max8(xs[c]) > thr[c];
+            need |= (kEight ? maximum8(xs[c]) : max8(xs[c])) > thr[c];
         }
         if (__any(need)) {
 #pragma unroll
             for (int c = 0; c < kNCT; ++c) {
-                float m = max8(xs[c]);
+                float m = kEight ? maximum8(xs[c]) : max8(xs[c]);
                 m = fmaxf(m, __shfl_xor(m, 16, 64));
                 m = fmaxf(m, __shfl_xor(m, 32, 64));
                 if constexpr (kFold) {
@@ -499,26 +581,19 @@ __device__ __forceinline__ void prefill_tile(
     // ---- prologue: the first kRing-1 steps of the range in flight, the first two landed,
     // scores of the first step, K operands of the second ----
     StepPages pg_next;                                            // pages of the step issued next
-    Codes codes;                                                  // 8-bit: the codes of the step stored next
     if constexpr (kEight) {
-        {
-            codes = fetch8(step_begin);
-            window8(step_begin + 1);
-            const Codes second = fetch8(step_begin + 1);
-            store8(step_begin, codes);
-            window8(step_begin + 2);
-            codes = fetch8(step_begin + 2);
-            store8(step_begin + 1, second);
-        }
+#pragma unroll
+        for (int j = 0; j < kAhead8 + 2; ++j) copy8(step_begin + j);
+        wait_vmcnt<kAhead8 * kLoads8>();
         __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+        widen8(step_begin);
+        widen8(step_begin + 1);
         load_k(step_begin);
         scores(std::true_type{}, step_begin, x);
         raise_max(x);
         load_k(step_begin + 1);
-        __syncthreads();                                          // every wavefront has read the slot of the first step's K
-        store8(step_begin + 2, codes);
-        window8(step_begin + 3);
-        codes = fetch8(step_begin + 3);
+        __syncthreads();                                          // V is there; every wavefront has read the first step's K
     } else {
 #pragma unroll
         for (int j = 0; j < kRing - 1; ++j) dma_step(step_begin + j, step_pages(step_begin + j));
@@ -538,8 +613,9 @@ __device__ __forceinline__ void prefill_tile(
     // i+2 are fetched and the new scores are tested against the running maxima.
     // kMask: causal / end-of-sequence masking (needed from the first edge step on);
     // kLast: there is no step i+1. ----
-    // From an 8-bit pool, the second half of iteration i also widens the codes of step i+3 (in the registers `codes`) into the
-    // slots that K(i+1) and V(i-1) left before the barrier, and sends for those of step i+4.
+    // From an 8-bit pool, iteration i sends for step i+2+kAhead8, and its second half also widens V(i+2) into the slot that V(i)
+    // left before the barrier.
+    bool saw_nan = false;
     auto iteration = [&](auto masked, auto last, int32_t i, float (&xc)[kNCT][8], float (&xn)[kNCT][8]) {
         constexpr bool kMask = decltype(masked)::value;
         constexpr bool kLast = decltype(last)::value;
@@ -554,7 +630,7 @@ __device__ __forceinline__ void prefill_tile(
             dma_step(i + kRing - 1, pg_next);
             pg_next = step_pages(i + kRing);           // consumed by the next iteration
         } else if (!kLast) {
-            window8(i + 4);
+            copy8(i + 2 + kAhead8);
         }
 
         if (!kLast) scores(masked, i + 1, xn);
@@ -568,7 +644,7 @@ __device__ __forceinline__ void prefill_tile(
                              : __builtin_amdgcn_exp2f(__builtin_fmaf(xc[c][j], scale_log2e, -m_run[c]));
             pb[c] = u32x4{ E::pack(p[0], p[1]), E::pack(p[2], p[3]), E::pack(p[4], p[5]), E::pack(p[6], p[7]) };
         }
-        const u32x4* vA = &lds_v[(uint32_t)i % kRing][0];
+        const u32x4* vA = &lds_v[(uint32_t)i % kSlotsV][0];
         // V slots at or past the end of the sequence hold stale bits (or nothing at all): zero
         // them so that a zero weight times the slot stays zero.  The lane's unit holds the 8
         // tokens 32*i + 16*(hi/2) + 8*(hi%2) + 0..7, two per dword.
@@ -586,10 +662,8 @@ __device__ __forceinline__ void prefill_tile(
             if (kMask) { av[dt][0] &= vm[0]; av[dt][1] &= vm[1]; av[dt][2] &= vm[2]; av[dt][3] &= vm[3]; }
         }
         if constexpr (kEight && kMask) {
-            // A V that is not a number must stay with the rows that see its token: a weight of zero would spread it.  Such values
-            // are replaced by zeros here, and put into the outputs of the rows that see one, feature by feature, by
-            // one more product of ones: where a NaN is, by where the mask lets the row look.  (Edge steps only: the
-            // others hide no key from a row.)
+            // A V that is not a number must stay with the rows that see its token: a weight of zero would spread it.  Here it
+            // becomes a zero; spread_nans() puts it where it belongs.  (Edge steps only: the others hide no key.)
             auto nans = [](uint32_t w) {                              // bit 15 of each half that is none
                 return ((w & 0x7fff7fffu) + (0x7fffu - E::kInfinity) * 0x00010001u) & 0x80008000u;
             };
@@ -599,57 +673,40 @@ __device__ __forceinline__ void prefill_tile(
 #pragma unroll
                 for (int e = 0; e < 4; ++e) any |= nans(av[dt][e]);
             if (__any(any != 0)) {
-                const int32_t key0 = i * kKeysPerStep + (lane >> 5) * 16 + ((lane >> 4) & 1) * 8;
-                u32x4 sees[kNCT];
+                saw_nan = true;
 #pragma unroll
-                for (int c = 0; c < kNCT; ++c)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        sees[c][e] = (key0 + 2 * e <= pos_q[c] ? E::kOnes & 0xffffu : 0u) | (key0 + 2 * e + 1 <= pos_q[c] ? E::kOnes & 0xffff0000u : 0u);
-#pragma unroll
-                for (int dt = 0; dt < D / 16; ++dt) {
-                    u32x4 there;
+                for (int dt = 0; dt < D / 16; ++dt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const uint32_t m = nans(av[dt][e]) >> 15;     // a one in each half
-                        there[e] = m * (E::kOnes & 0xffffu);
-                        av[dt][e] &= ~(m * 0xffffu);
+                        const uint32_t m = nans(av[dt][e]);
+                        av[dt][e] &= ~((m - (m >> 15)) | m);
                     }
-#pragma unroll
-                    for (int c = 0; c < kNCT; ++c) {
-                        const f32x4 hit = E::mfma32(there, sees[c], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[c][dt][e] = hit[e] > 0.f ? __builtin_nanf("") : o[c][dt][e];
-                    }
-                }
             }
         }
         if (!kMask && !kLast) {
             // steady state, first half: tell the scheduler the order we want.  The exp / convert
             // work of step i runs under the score MFMAs of step i+1, and the V operands are
             // fetched under them too.
-            constexpr int kQK = 2 * kNCT * (D / 32);
+            constexpr int kQK = 2 * kNCT * (kEight ? QCodes<D, E>::kProducts : D / 32);
             __builtin_amdgcn_sched_group_barrier(0x002, 4 * kNCT, 0);            // VALU
 #pragma unroll
             for (int r = 0; r < kQK; ++r) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);               // 1 MFMA
-                __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);               // 2 VALU
-                if (r < D / 16) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // V: one ds_read_b128
+                __builtin_amdgcn_sched_group_barrier(0x002, kEight ? 32 / kQK : 2, 0);   // 2 VALU (as many for all of them)
+                if (r * (kEight ? 16 / kQK : 1) < D / 16) __builtin_amdgcn_sched_group_barrier(0x100, kEight ? 16 / kQK : 1, 0);   // V: one ds_read_b128
             }
         }
         // K(i+2) and V(i+1) must have landed before anyone reads them: all but the copies of
         // the last kRing-3 steps issued
         __builtin_amdgcn_sched_barrier(0);             // nothing may move across the two halves
-        if constexpr (!kEight) wait_vmcnt<(kRing - 3) * kStepLoads>();
+        if constexpr (kEight) wait_vmcnt<kAhead8 * kLoads8>();
+        else wait_vmcnt<(kRing - 3) * kStepLoads>();
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
 
         if (kPriority) __builtin_amdgcn_s_setprio(kPriority);
         if (!kLast) load_k(i + 2);
-        if constexpr (kEight && !kLast) {
-            store8(i + 3, codes);
-            codes = fetch8(i + 4);
-        }
+        if constexpr (kEight && !kLast) widen8(i + 2);
 #pragma unroll
         for (int c = 0; c < kNCT; ++c)
             lacc[c] = E::mfma32(ones, pb[c], lacc[c]);
@@ -665,12 +722,51 @@ __device__ __forceinline__ void prefill_tile(
             constexpr int kPV = kNCT + kNCT * (D / 16);
 #pragma unroll
             for (int r = 0; r < kPV; ++r) {
+                if (kEight && r == 0) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);                 // the codes and the scale to widen
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
-                if (r >= 2 && r < 2 + 2 * (D / 32)) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // K: one ds_read_b128
+                __builtin_amdgcn_sched_group_barrier(0x002, kEight ? 2 : 1, 0);
+                if (r >= 2 && r < 2 + kRegsK + kEight) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // K: one ds_read_b128
+                if (kEight && r >= kPV - 2) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);           // what has been widened
             }
         }
         if (!kLast) raise_max(xn);
+    };
+    // 8-bit pools, where an edge step held a V that is not a number: the outputs that see it become NaN, feature by feature, by a
+    // product of ones -- where the V is none, by where the mask lets a row look.  The codes are read again from the pool.
+    auto spread_nans = [&]() {
+        for (int32_t step = max(step_begin, min(first_edge, step_end - 1)); step < step_end; ++step) {
+            const int32_t entry = kStepPages * step + (lane >> 5), key0 = step * kKeysPerStep + (lane >> 5) * 16 + ((lane >> 4) & 1) * 8;
+            const int32_t id = entry < n_pages ? table[entry] : 0;
+            const char* v = (const char*)layer_base + (int64_t)((id < 0 || id >= num_pages) ? 0 : id) * page_stride * 2
+                          + (Hkv + g) * (PS * D) + (lane & 15) * 16;
+#pragma unroll
+            for (int u = 0; u < D / 64; ++u) {
+                // this lane's 8 tokens of features u*64 + 16 e + lane%16: byte e*4 + token%4 of two units
+                u32x4 w[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) w[h] = *(const u32x4*)(v + (u * 4 + ((lane >> 4) & 1) * 2 + h) * 256);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    u32x4 there;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t pair = w[j >> 1][e] >> (16 * (j & 1));
+                        there[j] = ((pair & 0x7fu) == 0x7fu && key0 + 2 * j < n_seq_keys ? E::kOnes & 0xffffu : 0u)
+                                 | ((pair & 0x7f00u) == 0x7f00u && key0 + 2 * j + 1 < n_seq_keys ? E::kOnes & 0xffff0000u : 0u);
+                    }
+#pragma unroll
+                    for (int c = 0; c < kNCT; ++c) {
+                        u32x4 sees;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            sees[j] = (key0 + 2 * j <= pos_q[c] ? E::kOnes & 0xffffu : 0u) | (key0 + 2 * j + 1 <= pos_q[c] ? E::kOnes & 0xffff0000u : 0u);
+                        const f32x4 hit = E::mfma32(there, sees, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[c][u * 4 + e][i] = hit[i] > 0.f ? __builtin_nanf("") : o[c][u * 4 + e][i];
+                    }
+                }
+            }
+        }
     };
     float xb[kNCT][8];
     int32_t i = step_begin;
@@ -689,6 +785,9 @@ __device__ __forceinline__ void prefill_tile(
     iteration(std::true_type{}, std::true_type{}, i, x, xb);
     if (kPriority) __builtin_amdgcn_s_setprio(0);
     wait_vmcnt<0>();                                   // no copy may outlive the workgroup's LDS
+    if constexpr (kEight) {
+        if (saw_nan) spread_nans();
+    }
 
     // ---- a cut tile leaves the partial of its range: unnormalised output, running max and sum per
     // query row ----
