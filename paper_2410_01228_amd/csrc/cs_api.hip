@@ -134,6 +134,11 @@ static void plan_decode_loads(const cs_batch* b, DecodePlan& p, int32_t Hkv, int
     p.counted_loads = p.in_args && (wgs <= cus || (p.longest < 512 ? shares >= 0.9 : shares >= 1.1 && beside <= 0.58));
     if (p.counted_loads && p.longest >= 1024 && shares >= 1.25 && beside <= 0.5) p.pages_ahead = 2;
     // (a depth asked for is that of the form for full chips)
+    if (p.elem_bytes == 1) {                                // (decode_item8 has one form)
+        p.pages_ahead = 1;
+        p.counted_loads = p.in_args;
+        return;
+    }
     const int32_t forced = g_forced_ahead.load();
     if (forced == 1 || forced == 2) {
         p.pages_ahead = forced;
@@ -176,8 +181,10 @@ DecodePlan plan_decode(const cs_batch* b, int32_t Hkv, int32_t head_dim, int32_t
         // per CU (over 171 random batches of three shapes: mean distance to the best forced plan
         // 3.8% -> 2.3%, worst 61% -> 17%, together with the floor rule below).
         // (the workgroup counts and byte volumes below were measured on 256 CUs and scale with the chip)
-        const int32_t cap = head_dim >= 128 ? 4096 : 8192;
-        const int64_t kv_bytes = p.decode_keys * 2 * Hkv * head_dim * elem_bytes;
+        // 8-bit pools: items of 8192 keys at either head dim (128 decodes of 2K-32K keys, 64/8 heads, 768 -> 751 us), everything
+        // else as for the same keys in 16 bits (64 of 1K-8K, 28/4: pieces of 1024 instead of 2048, 61.3 -> 58.8).
+        const int32_t cap = head_dim >= 128 && elem_bytes == 2 ? 4096 : 8192;
+        const int64_t kv_bytes = p.decode_keys * 2 * Hkv * head_dim * 2;
         const int64_t need = p.uniform ? cus : kv_bytes >= 400000000ll * cus / 256 ? 3 * cus : cus * 3 / 2;
         auto workgroups_at = [&](int32_t sp) {
             int64_t items = 0;

@@ -70,7 +70,7 @@ __device__ __forceinline__ void split_workgroup(
     const DecodePartials mine = part.of_layer(blockIdx.y, n_items, Hkv * G, Hkv, D);
     out += blockIdx.y * next_q;
     if constexpr (E::kEightBit)
-        decode_item8<D, Src, E, kAhead, kLoads>(lds, layer_base + blockIdx.y * next_layer, page_stride, num_pages, Hkv, G, block_tables, max_blocks, src, ctx_lens,
+        decode_item8<D, Src, E>(lds, layer_base + blockIdx.y * next_layer, page_stride, num_pages, Hkv, G, block_tables, max_blocks, src, ctx_lens,
                            cu_q_lens, q + blockIdx.y * next_q, out, scale_log2e, mine, item, g);
     else
         decode_item<D, Src, E, kAhead, PS, kLoads>(lds, layer_base + blockIdx.y * next_layer, page_stride, num_pages, Hkv, G, block_tables, max_blocks, src, ctx_lens,
@@ -130,7 +130,7 @@ static int launch_decode_as(const cs_kv_pool& pool, int32_t layer, const LayerSp
                             bool merge_only)
 {
     if (plan.num_decode == 0) return CS_OK;
-    constexpr int kOtherPage = E::kEightBit ? 16 : 8;                  // (8-bit pools have pages of 16 only)
+    constexpr int kOtherPage = E::kEightBit ? 16 : 8, kDeep = E::kEightBit ? 1 : 2;   // (8-bit pools have pages of 16 only, and one form of the kernel)
     const int32_t Hkv = pool.num_kv_heads, D = pool.head_dim, G = Hq / Hkv;
     const uint16_t* layer_base = (const uint16_t*)pool.base + (int64_t)layer * pool.layer_stride;
     const float scale_log2e = scale * 1.4426950408889634f;
@@ -149,9 +149,10 @@ static int launch_decode_as(const cs_kv_pool& pool, int32_t layer, const LayerSp
 #define CS_LAUNCH_DECODE_A(KERNEL, DD, SRC, src, AH, CUT)                                                    \
     if (pool.page_size == 16) { CS_LAUNCH_DECODE_P(KERNEL, DD, SRC, src, AH, 16, CUT) } else { CS_LAUNCH_DECODE_P(KERNEL, DD, SRC, src, AH, kOtherPage, CUT) }
 #define CS_LAUNCH_DECODE(KERNEL, DD, SRC, src, CUT)                                                         \
-    if (plan.pages_ahead == 2) { CS_LAUNCH_DECODE_A(KERNEL, DD, SRC, src, 2, CUT) } else { CS_LAUNCH_DECODE_A(KERNEL, DD, SRC, src, 1, CUT) }
+    if (plan.pages_ahead == 2) { CS_LAUNCH_DECODE_A(KERNEL, DD, SRC, src, kDeep, CUT) } else { CS_LAUNCH_DECODE_A(KERNEL, DD, SRC, src, 1, CUT) }
 #define CS_LAUNCH_DECODE_ARGS(DD, CUT)                                                                      \
-    if (plan.counted_loads) { CS_LAUNCH_DECODE(decode_lone_kernel, DD, ItemsInArgs, plan.arg_items, CUT) } else { CS_LAUNCH_DECODE(decode_split_kernel, DD, ItemsInArgs, plan.arg_items, CUT) }
+    if constexpr (E::kEightBit) { CS_LAUNCH_DECODE(decode_split_kernel, DD, ItemsInArgs, plan.arg_items, CUT) }                      \
+    else if (plan.counted_loads) { CS_LAUNCH_DECODE(decode_lone_kernel, DD, ItemsInArgs, plan.arg_items, CUT) } else { CS_LAUNCH_DECODE(decode_split_kernel, DD, ItemsInArgs, plan.arg_items, CUT) }
 #define CS_LAUNCH_MERGE(DD, SRC, src)                                                                       \
     hipLaunchKernelGGL((decode_merge_kernel<DD, SRC, typename E::Wide>), grid, dim3(kDecodeThreads), 0, st, Hkv, G, src, b.ctx_lens, \
                        b.cu_q_lens, (uint16_t*)out, part, span.q);

@@ -120,9 +120,15 @@ __device__ __forceinline__ void process_step8(WaveState<D>& st, const StepRegs8<
         }
 }
 
-// decode_item for 8-bit pools: page_stride in units of 2 bytes; kAhead: steps a wavefront keeps in flight beyond the one it
-// multiplies.
-template <int D, class Src, class E, int kAhead, Loads kLoads>
+// decode_item for 8-bit pools: page_stride in units of 2 bytes.
+//
+// One form for every launch: a step ahead, with loads that the compiler can count (Loads::kLone there).  A workgroup
+// takes half as long as over 16-bit pages, so more of a launch is the time of its last ones, alone on their CUs, and full chips
+// do not mind: skipped loads, one step ahead, 256 decodes of 512-4096 keys, 32/8 heads, 194.6 us, this 192.3; of 1000-8000, 4/2
+// heads, 90 and 64; 8 of 128-2048 uncut, 32/8, 24.9 and 18.0.  Two steps ahead are within 0.3% on full chips, up to 8% faster for a
+// few long items (1 of 20000, 64/8, pieces of 1024: 18.5 us instead of 19.9) and 1-18% slower for many short ones (300 of
+// 50-500: 48.7 instead of 41.2).  Four workgroups a CU, in 128 registers, spill: 244 us.
+template <int D, class Src, class E>
 __device__ __forceinline__ void decode_item8(
     DecodeLds<D>& lds,
     const uint16_t* __restrict__ layer_base, int64_t page_stride, int32_t num_pages,
@@ -167,58 +173,28 @@ __device__ __forceinline__ void decode_item8(
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) st.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    static_assert(kAhead == 1 || kAhead == 2, "one or two steps ahead");
     const char* base = (const char*)layer_base;
     const int64_t page_bytes = page_stride * 2;
-    auto fetch = [&](StepRegs8<D>& r, const StepIds<8>& id) {
-        if constexpr (kLoads != Loads::kSkipped) {
-            load_step8<D>(r, base, page_bytes, loadable<8>(id, num_pages), g, Hkv, lane);
-        } else {
-            if (step_ok<8>(id, num_pages)) load_step8<D>(r, base, page_bytes, id, g, Hkv, lane);
-        }
-    };
     auto id_at = [&](int32_t p) { return step_ids8(table, p, page_end); };
+    auto fetch = [&](StepRegs8<D>& r, const StepIds<8>& id) { load_step8<D>(r, base, page_bytes, loadable<8>(id, num_pages), g, Hkv, lane); };
     auto use = [&](const StepRegs8<D>& r, const StepIds<8>& id, int32_t pg) {
         if (step_ok<8>(id, num_pages)) process_step8<D, E>(st, r, qb, scale_log2e, pg << 4, end_key, lane);
     };
     constexpr int kStride = 2 * kDecodeWaves;                              // pages from a wavefront's step to its next
     int32_t pg = page_begin + 2 * wave;                                    // wave w takes the steps w, w + 4, ...
-    if constexpr (kAhead == 1) {
-        StepRegs8<D> cur, nxt;
-        StepIds<8> id_cur = id_at(pg);
-        StepIds<8> id_nxt = id_at(pg + kStride);
-        constexpr int kPeeled = kLoads == Loads::kLone ? kStride : 0;      // (the wavefront's last step)
-        if (kPeeled == 0 || pg < page_end) fetch(cur, id_cur);
-        while (pg + kPeeled < page_end) {
-            const StepIds<8> id_n2 = id_at(pg + 2 * kStride);
-            fetch(nxt, id_nxt);
-            use(cur, id_cur, pg);
-            cur = nxt;
-            id_cur = id_nxt;
-            id_nxt = id_n2;
-            pg += kStride;
-        }
-        if (kPeeled != 0 && pg < page_end) use(cur, id_cur, pg);
-    } else {
-        StepRegs8<D> b0, b1, b2;
-        StepIds<8> id0 = id_at(pg), id1 = id_at(pg + kStride), id2 = id_at(pg + 2 * kStride);
-        fetch(b0, id0);
-        fetch(b1, id1);
-        auto stage = [&](StepRegs8<D>& now, StepRegs8<D>& fill) {
-            const StepIds<8> id3 = id_at(pg + 3 * kStride);
-            fetch(fill, id2);
-            use(now, id0, pg);
-            id0 = id1; id1 = id2; id2 = id3;
-            pg += kStride;
-        };
-        while (pg < page_end) {
-            stage(b0, b2);
-            if (pg >= page_end) break;
-            stage(b1, b0);
-            if (pg >= page_end) break;
-            stage(b2, b1);
-        }
+    StepRegs8<D> cur, nxt;
+    StepIds<8> id_cur = id_at(pg), id_nxt = id_at(pg + kStride);
+    if (pg < page_end) fetch(cur, id_cur);
+    while (pg + kStride < page_end) {
+        const StepIds<8> id_n2 = id_at(pg + 2 * kStride);
+        fetch(nxt, id_nxt);
+        use(cur, id_cur, pg);
+        cur = nxt;
+        id_cur = id_nxt;
+        id_nxt = id_n2;
+        pg += kStride;
     }
+    if (pg < page_end) use(cur, id_cur, pg);                               // the wavefront's last step: nothing is loaded behind it
     leave_item<D, E>(lds, st, it, t, item, g, Hq, G, out, part, lane, wave);
 }
 

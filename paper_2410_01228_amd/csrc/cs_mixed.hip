@@ -91,7 +91,7 @@ __global__ __launch_bounds__(kPrefillThreads, 2) void mixed_kernel(
             // with a tile must stream by itself); a deeper queue only delays the tile's own
             // copies, which share the CU's memory pipeline
             if constexpr (E::kEightBit)
-                decode_item8<D, ItemsInArgs, E, 1, Loads::kCounted>(lds.decode, layer_base + l * next_layer, page_stride, num_pages, Hkv, G, block_tables,
+                decode_item8<D, ItemsInArgs, E>(lds.decode, layer_base + l * next_layer, page_stride, num_pages, Hkv, G, block_tables,
                                            max_blocks, items, ctx_lens, cu_q_lens, q + l * next_q, out + l * next_q, scale_log2e,
                                            mine, item, g);
             else
