@@ -23,24 +23,31 @@ constexpr float kMostHalf = 61440.f;         // the largest value of 4 significa
 // Where the blocks' scales begin in a page, in bytes.
 __host__ __device__ inline int32_t scales_offset(int32_t Hkv, int32_t D) { return 2 * Hkv * (kPage * D); }
 
-// The new rows' element type.
+// The new rows' element type.  kMost: a block whose largest value is beyond it is a rare one (rare_top, rare_code): bf16
+// infinities, which end at the largest code and say nothing about the scale; fp16 values beyond kMostHalf, which end there.
 struct RowBf16 {
+    static constexpr float kMost = 3.4e38f;
+    static constexpr uint32_t kMostBits = 0x7f7f;
+    static __device__ __forceinline__ float value(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
     static __device__ __forceinline__ void widen(uint32_t w, float& a, float& b) {
         a = __builtin_bit_cast(float, w << 16);
         b = __builtin_bit_cast(float, w & 0xffff0000u);
     }
-    // (infinities end at the largest code and say nothing about the scale)
-    static __device__ __forceinline__ float size(float x) { x = fabsf(x); return x <= 3.4e38f ? x : 0.f; }
+    static __device__ __forceinline__ float rare_size(float x) { return fabsf(x) <= kMost ? fabsf(x) : 0.f; }
+    static __device__ __forceinline__ float rare_limit(float) { return kMostCode; }
 };
 struct RowF16 {
     typedef _Float16 x2 __attribute__((ext_vector_type(2)));
-    static __device__ __forceinline__ float clamp(float x) { return x != x ? x : fminf(fmaxf(x, -kMostHalf), kMostHalf); }
+    static constexpr float kMost = kMostHalf;
+    static constexpr uint32_t kMostBits = 0x7b80;
+    static __device__ __forceinline__ float value(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
     static __device__ __forceinline__ void widen(uint32_t w, float& a, float& b) {
         const x2 v = __builtin_bit_cast(x2, w);
-        a = clamp((float)v[0]);
-        b = clamp((float)v[1]);
+        a = (float)v[0];
+        b = (float)v[1];
     }
-    static __device__ __forceinline__ float size(float x) { x = fabsf(x); return x == x ? x : 0.f; }
+    static __device__ __forceinline__ float rare_size(float x) { return x == x ? fminf(fabsf(x), kMost) : 0.f; }
+    static __device__ __forceinline__ float rare_limit(float inv) { return kMostHalf * inv; }
 };
 
 __device__ __forceinline__ float power(int32_t e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
@@ -54,13 +61,49 @@ __device__ __forceinline__ int32_t exponent_of(float scale) {
     return min(max((int32_t)((__builtin_bit_cast(uint32_t, scale) >> 23) & 255) - 127, kLeastExponent), kMostExponent);
 }
 
-// Two values over the scale as two codes (bits 0-15).
-__device__ __forceinline__ uint32_t codes2(float a, float b, float inv) {
-    a *= inv;
-    b *= inv;
-    if (fabsf(a) > kMostCode) a = copysignf(kMostCode, a);       // infinities only; a NaN stays one
-    if (fabsf(b) > kMostCode) b = copysignf(kMostCode, b);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xffffu;
+// Scaled values of a rare block: none beyond the largest code that it may use; NaN stays NaN.
+template <class Row, int N>
+__device__ __forceinline__ void limit(float (&x)[N], float inv) {
+    const float most = Row::rare_limit(inv);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (fabsf(x[i]) > most) x[i] = copysignf(most, x[i]);
+}
+// The largest size among N words of two values, over the wavefront, and whether the block is a rare one.  Sizes of either type
+// order like their bits, two at a time; beyond kMostBits come values beyond kMost, infinities and NaNs (which are no maximum).
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <class Row, int N>
+__device__ __forceinline__ float largest(const uint32_t (&w)[N], bool& rare) {
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    uint32_t bits = max((uint32_t)m[0], (uint32_t)m[1]);
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, k, 64));
+    rare = bits > Row::kMostBits;
+    if (!rare) return Row::value(bits);
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float a, b;
+        Row::widen(w[i], a, b);
+        top = fmaxf(top, fmaxf(Row::rare_size(a), Row::rare_size(b)));
+    }
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
+    return top;
+}
+// Four values over the scale as four codes.
+template <class Row>
+__device__ __forceinline__ uint32_t codes4(uint32_t w0, uint32_t w1, float inv, bool rare) {
+    float x[4];
+    Row::widen(w0, x[0], x[1]);
+    Row::widen(w1, x[2], x[3]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] *= inv;
+    if (rare) limit<Row>(x, inv);
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], lo, true);
 }
 // Four codes at a scale that is `factor` of theirs.
 __device__ __forceinline__ uint32_t rescale4(uint32_t w, float factor) {
@@ -78,9 +121,16 @@ __device__ __forceinline__ uint32_t first_bytes(int32_t n) {
 
 constexpr int kAppend8SlotShift = 4;
 
-// Chunks.  A workgroup of 2 D threads owns one (page touched this step, kv head): the lower half its K block, the upper half its
-// V block, a thread 16 features of one token.  Bound by memory (three bytes a value): rows come in 16 bytes a lane, the codes
-// leave as whole 16-byte units; V goes through LDS, where it is turned from 16 features of a token to 4 tokens of 4.
+constexpr int kAppend8Threads = 128;
+
+// Chunks.  A workgroup owns one (page touched this step, kv head), one wavefront its K block, the other its V block; a lane has 16
+// features of a token, at head dim 128 twice.  Bound by memory (three bytes a value) and, below some thousand tokens, by the
+// trips to it: lengths, then rows, table entry and what the page holds.  Rows come in 16 bytes a lane, the codes leave as whole
+// 16-byte units; V goes through LDS, where it is turned from 16 features of a token to 4 tokens of 4.  The wavefronts need
+// nothing of each other: no barrier, and twice as many bytes under way as with a block shared by two of them (2048 tokens, 8
+// heads, 5.4 -> 4.8 us; 31200 tokens 42.9 -> 40.8).  Rows are loaded through the caches: they come from a projection just done, which
+// leaves them in the last level (31200 tokens 41.0 -> 31.4 us, 6.1 TB/s; 128 single tokens + 9900 in chunks 15.3 -> 12.0).  Two or four
+// heads a workgroup are slower below some 10000 tokens (512: 3.7, 4.5, 6.6 us).
 // Workgroup slots are dealt to sequences as start(s) = cu_q_lens[s]/16 + 2s, as in the 16-bit append.
 template <class Row, int D>
 __device__ __forceinline__ void append8_page(
@@ -88,9 +138,9 @@ __device__ __forceinline__ void append8_page(
     const int32_t* __restrict__ block_tables, int32_t max_blocks, const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ cu_q_lens,
     const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new)
 {
+    constexpr int kUnits = D / 64;
     constexpr int kRowBytes = D + 16;                              // LDS row of a token's codes: 4 rows start 16 banks apart
     __shared__ __attribute__((aligned(16))) uint8_t turned[kPage * kRowBytes];
-    __shared__ float tops[4];
     const int32_t per = 8 * Hkv, group = block / per, in_group = block - group * per;   // a page's heads on one XCD
     const int32_t h = in_group >> 3, slot_id = base_slot + group * 8 + (in_group & 7);
     const OwnedBy own = owner_of(cu_q_lens, ctx_lens, first_seq, S - first_seq, slot_id, [](int32_t t, int32_t i) { return (t >> kAppend8SlotShift) + 2 * i; });
@@ -99,76 +149,77 @@ __device__ __forceinline__ void append8_page(
     const int32_t blk = (first >> 4) + (slot_id - ((own.token >> kAppend8SlotShift) + 2 * own.seq));
     const int32_t p0 = blk << 4;
     if (p0 >= last || blk >= max_blocks) return;
-    const bool is_v = threadIdx.x >= D;
-    const int32_t idx = threadIdx.x & (D - 1), tok = idx & 15, fb = idx >> 4, lane = threadIdx.x & 63;
+    const bool is_v = threadIdx.x >= 64;
+    const int32_t lane = threadIdx.x & 63, tok = lane & 15;
     const int32_t page = block_tables[(int64_t)own.seq * max_blocks + blk];
     const int32_t pos = p0 + tok;
     const bool is_new = pos >= first && pos < last;
-    u32x4 w[2] = {u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}};
-    if (is_new) {
-        const uint16_t* src = (is_v ? v_new : k_new) + ((int64_t)(own.token + pos - first) * Hkv + h) * D + fb * 16;
-        w[0] = __builtin_nontemporal_load((const u32x4*)src);
-        w[1] = __builtin_nontemporal_load((const u32x4*)src + 1);
+    uint32_t w[8 * kUnits];
+    const uint16_t* src = (is_v ? v_new : k_new) + ((int64_t)(own.token + pos - first) * Hkv + h) * D + (lane >> 4) * 16;
+#pragma unroll
+    for (int i = 0; i < 2 * kUnits; ++i) {
+        u32x4 r = {0u, 0u, 0u, 0u};
+        if (is_new) r = ((const u32x4*)(src + (i >> 1) * 64))[i & 1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[4 * i + j] = r[j];
     }
-    const bool page_ok = page >= 0 && page < num_pages;            // (the same in every thread)
-    char* page_base = layer_base + (int64_t)(page_ok ? page : 0) * page_bytes;
-    u32x4* unit = (u32x4*)(page_base + ((is_v ? Hkv : 0) + h) * (kPage * D)) + idx;
+    const bool page_ok = page >= 0 && page < num_pages;
+    if (!page_ok) return;
+    char* page_base = layer_base + (int64_t)page * page_bytes;
+    u32x4* unit = (u32x4*)(page_base + ((is_v ? Hkv : 0) + h) * (kPage * D)) + lane;
     float* scale = (float*)(page_base + scales_offset(Hkv, D)) + (is_v ? Hkv : 0) + h;
     const int32_t held = min(max(first - p0, 0), kPage);           // tokens that the page holds already
     const int32_t upto = min(last - p0, kPage);
-    // (what the block holds is asked for beside the rows)
-    const bool partial = page_ok && (held > 0 || upto < kPage);
-    u32x4 old = {0u, 0u, 0u, 0u};
+    // (what the block holds is asked for while the rows are on their way)
+    u32x4 old[kUnits];
     float old_scale = 0.f;
-    if (partial && (is_v || held > 0)) old = *unit;
-    if (page_ok && held > 0) old_scale = *scale;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        old[u] = u32x4{0u, 0u, 0u, 0u};
+        if (is_v ? held > 0 || upto < kPage : held > 0) old[u] = unit[u * 64];
+    }
+    if (held > 0) old_scale = *scale;
 
-    float x[16], top = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        Row::widen(w[i >> 2][i & 3], x[2 * i], x[2 * i + 1]);
-        top = fmaxf(top, fmaxf(Row::size(x[2 * i]), Row::size(x[2 * i + 1])));
-    }
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
-    if (D == 128) {
-        if (lane == 0) tops[threadIdx.x >> 6] = top;
-        __syncthreads();
-        top = fmaxf(tops[is_v ? 2 : 0], tops[is_v ? 3 : 1]);
-    }
+    bool rare;
+    const float top = largest<Row>(w, rare);
     int32_t e = exponent_for(top);
     const int32_t e_old = exponent_of(old_scale);
     if (held > 0) e = max(e, e_old);
     const float inv = power(-e);
-    u32x4 c;
+    u32x4 c[kUnits];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        c[i] = codes2(x[4 * i], x[4 * i + 1], inv) | (codes2(x[4 * i + 2], x[4 * i + 3], inv) << 16);
+    for (int i = 0; i < 4 * kUnits; ++i) c[i >> 2][i & 3] = codes4<Row>(w[2 * i], w[2 * i + 1], inv, rare);
     const bool raised = held > 0 && e > e_old;
     const float factor = rescale_factor(e_old, e);
-    if (is_v) *(u32x4*)(turned + tok * kRowBytes + fb * 16) = c;
-    __syncthreads();
-    if (!page_ok) return;
     if (!is_v) {
-        if (is_new) *unit = c;
-        else if (raised && tok < held) *unit = u32x4{rescale4(old[0], factor), rescale4(old[1], factor), rescale4(old[2], factor), rescale4(old[3], factor)};
-    } else {
-        // unit idx: tokens 4 tg .. +4 of features dq*64 + 16 i + f
-        const int32_t f = idx & 15, tg = (idx >> 4) & 3, dq = idx >> 6;
-        const uint8_t* from = turned + 4 * tg * kRowBytes + dq * 64 + f;
-        const uint32_t below = first_bytes(held - 4 * tg), fresh = first_bytes(upto - 4 * tg) & ~below;
-        u32x4 n;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t v = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v |= (uint32_t)from[j * kRowBytes + i * 16] << (8 * j);
-            const uint32_t before = raised ? (rescale4(old[i], factor) & below) | (old[i] & ~below) : old[i];
-            n[i] = (v & fresh) | (before & ~fresh);
+        for (int u = 0; u < kUnits; ++u) {
+            if (is_new) unit[u * 64] = c[u];
+            else if (raised && tok < held)
+                unit[u * 64] = u32x4{rescale4(old[u][0], factor), rescale4(old[u][1], factor), rescale4(old[u][2], factor), rescale4(old[u][3], factor)};
         }
-        if (fresh != 0 || (raised && below != 0)) *unit = n;
+    } else {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) *(u32x4*)(turned + tok * kRowBytes + (u * 4 + (lane >> 4)) * 16) = c[u];
+        // unit u*64 + lane: tokens 4 tg .. +4 of features u*64 + 16 i + f (a wavefront's LDS accesses stay in order)
+        const int32_t f = lane & 15, tg = lane >> 4;
+        const uint32_t below = first_bytes(held - 4 * tg), fresh = first_bytes(upto - 4 * tg) & ~below;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const uint8_t* from = turned + 4 * tg * kRowBytes + u * 64 + f;
+            u32x4 n;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t v = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v |= (uint32_t)from[j * kRowBytes + i * 16] << (8 * j);
+                const uint32_t before = raised ? (rescale4(old[u][i], factor) & below) | (old[u][i] & ~below) : old[u][i];
+                n[i] = (v & fresh) | (before & ~fresh);
+            }
+            if (fresh != 0 || (raised && below != 0)) unit[u * 64] = n;
+        }
     }
-    if (idx == 0 && (held == 0 || raised)) *scale = power(e);
+    if (lane == 0 && (held == 0 || raised)) *scale = power(e);
 }
 
 // Single tokens (decode): a wavefront per (sequence, kv head), a lane D/64 features of K and of V.  Bound by latency: lengths,
@@ -206,16 +257,14 @@ __device__ __forceinline__ void append8_token(
     bool raised[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-        float x0, x1;
-        Row::widen(word[b], x0, x1);
-        float top = D == 128 ? fmaxf(Row::size(x0), Row::size(x1)) : Row::size(x0);
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
+        const uint32_t w[1] = {word[b]};
+        bool rare;
+        const float top = largest<Row>(w, rare);
         e[b] = exponent_for(top);
         e_old[b] = exponent_of(old[b]);
         raised[b] = slot > 0 && e[b] > e_old[b];
         if (slot > 0) e[b] = max(e[b], e_old[b]);
-        code[b] = codes2(x0, x1, power(-e[b]));
+        code[b] = codes4<Row>(word[b], 0u, power(-e[b]), rare);
         if (lane == 0 && (slot == 0 || raised[b])) scale[b * Hkv] = power(e[b]);
     }
     char* kblk = page_base + h * (kPage * D);
@@ -262,7 +311,7 @@ __device__ __forceinline__ void append8_token(
 
 // Chunks first, single tokens behind them, in one launch.
 template <class Row, int D>
-__global__ __launch_bounds__(2 * D) void append8_kernel(
+__global__ __launch_bounds__(kAppend8Threads) void append8_kernel(
     char* __restrict__ layer_base, int64_t page_bytes, int32_t num_pages, int32_t Hkv, int32_t S, int32_t chunk_seq, int32_t base_slot,
     int32_t single_seq, int32_t single_end, const int32_t* __restrict__ block_tables, int32_t max_blocks,
     const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ cu_q_lens,
@@ -272,7 +321,7 @@ __global__ __launch_bounds__(2 * D) void append8_kernel(
         append8_page<Row, D>((int32_t)blockIdx.x, layer_base, page_bytes, num_pages, Hkv, S, chunk_seq, base_slot, block_tables, max_blocks,
                              ctx_lens, cu_q_lens, k_new, v_new);
     else
-        append8_token<Row, D>((int32_t)((blockIdx.x - page_blocks) * (2 * D / 64) + (threadIdx.x >> 6)), layer_base, page_bytes, num_pages, Hkv,
+        append8_token<Row, D>((int32_t)((blockIdx.x - page_blocks) * (kAppend8Threads / 64) + (threadIdx.x >> 6)), layer_base, page_bytes, num_pages, Hkv,
                               single_seq, single_end, block_tables, max_blocks, ctx_lens, cu_q_lens, k_new, v_new);
 }
 
@@ -311,12 +360,12 @@ static int append8(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch
     }
     const int32_t base_slot = chunk0 < 0 ? 0 : (b.h_cu_q_lens[chunk0] >> kAppend8SlotShift) + 2 * chunk0;
     const int64_t slots = chunk0 < 0 ? 0 : ((int64_t)(b.h_cu_q_lens[chunk1] >> kAppend8SlotShift) + 2 * chunk1 - base_slot + 7) & ~7ll;
-    const int64_t page_blocks = slots * Hkv, waves = 2 * D / 64;
+    const int64_t page_blocks = slots * Hkv, waves = kAppend8Threads / 64;
     const int64_t token_blocks = single0 < 0 ? 0 : ((int64_t)(single1 - single0) * Hkv + waves - 1) / waves;
-    if ((page_blocks + token_blocks) * 2 * D > 4294967295ll) return CS_ERR_UNSUPPORTED;    // lanes of a launch
+    if ((page_blocks + token_blocks) * kAppend8Threads > 4294967295ll) return CS_ERR_UNSUPPORTED;    // lanes of a launch
     char* base = (char*)pool->base + (int64_t)layer * pool->layer_stride;
 #define CS_LAUNCH_APPEND8(ROW, DD)                                                                                      \
-    hipLaunchKernelGGL((append8_kernel<ROW, DD>), dim3((uint32_t)(page_blocks + token_blocks)), dim3(2 * DD), 0, (hipStream_t)stream, base, \
+    hipLaunchKernelGGL((append8_kernel<ROW, DD>), dim3((uint32_t)(page_blocks + token_blocks)), dim3(kAppend8Threads), 0, (hipStream_t)stream, base, \
                        pool->page_stride, pool->num_pages, Hkv, chunk1, chunk0, base_slot, single0, single1, b.block_tables,     \
                        b.max_blocks_per_seq, b.ctx_lens, b.cu_q_lens, (const uint16_t*)k_new, (const uint16_t*)v_new, (uint32_t)page_blocks);
     if (D == 128) { if (f16) { CS_LAUNCH_APPEND8(RowF16, 128) } else { CS_LAUNCH_APPEND8(RowBf16, 128) } }

@@ -92,7 +92,8 @@ __global__ __launch_bounds__(kLanes) void pages_fork_kernel(const Pages pool, in
                                                             const int32_t* __restrict__ parents, const int32_t* __restrict__ children,
                                                             const int32_t* __restrict__ fresh_pages, int32_t n_forks)
 {
-    // neighbours in the list on one XCD: they often have the same parent, whose page then comes from its L2
+    // neighbours in the list on one XCD: they often have the same parent, whose page then comes from its L2 (64 parents, 8 children each,
+    // 80 layers of 32832 bytes: 489 -> 252 us)
     int32_t i, c;
     deal(blockIdx.x, chunks_per_page, i, c);
     i = (i & (kXcds - 1)) * (int32_t)(gridDim.x / ((uint32_t)chunks_per_page * kXcds)) + i / kXcds;
