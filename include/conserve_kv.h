@@ -2,7 +2,8 @@
  * conserve_kv.h -- C ABI of the MI355X (gfx950) kernels for the per-layer GPU hot path of
  * online/offline LLM co-serving: KV append, paged attention over a mixed batch of decode
  * and chunked-prefill tokens, and the gather / restore copies of incremental KV
- * checkpointing (paper Sec. 4.2, 4.3, 4.4, 5).
+ * checkpointing (paper Sec. 4.2, 4.3, 4.4, 5); the first two over a cache of 8-bit codes
+ * too, and the copies, forks, frees and compaction of whole pages of either.
  *
  * Conventions for every call
  *   - returns a cs_status (0 = CS_OK, negative = error); all checks that need only host
@@ -19,7 +20,8 @@
  *   - every pointer is owned by the caller and must stay valid until the enqueued work has
  *     run.  "device" pointers are HIP device memory of the current device, "host" pointers
  *     are ordinary host memory read during the call only;
- *   - 16-bit data (bf16; fp16 through cs_paged_attention_mixed_f16), 16 tokens per page (the
+ *   - 16-bit data (bf16; fp16 through cs_paged_attention_mixed_f16; K and V in 8 bits through the
+ *     cs_kv8_ calls), 16 tokens per page (the
  *     paper's page granularity, Sec. 5) or 8 (cs_kv_pool.page_size), head_dim 64 or 128,
  *     num_q_heads / num_kv_heads <= 16;
  *   - each call works on ONE decoder layer (attention, append) or a layer range (gather,
@@ -28,7 +30,7 @@
  *     num_tokens with the same arrays drops the offline tail without rebuilding metadata;
  *   - device index arrays (block tables, page id lists) are not validated on the host (that
  *     would need a synchronisation).  A page id outside [0, num_pages) is never dereferenced:
- *     the copies (append, gather, restore) skip it.  The attention output of a sequence whose
+ *     the copies (append, gather, restore, page copies and forks) skip it.  The attention output of a sequence whose
  *     block table holds such an id within its length is unspecified (the decode path leaves
  *     the page's keys out and writes zeros if no key is left; the chunk path reads page 0 of
  *     the pool in its place); every other sequence of the batch is unaffected;
@@ -380,8 +382,8 @@ size_t cs_kv8_page_bytes(int32_t num_kv_heads, int32_t head_dim);
  * unless they fall below 2^-6 of the new scale).  Pages that are full never change, slots behind the last
  * token are left as they are, and a token's code depends only on its own value and its block's scale.
  * Infinities do not count for e and end as the largest code; a NaN stays one.  fp16: values beyond 61440, the
- * largest multiple of an e4m3 value that half precision holds, are rounded to it.  A block must not be appended to by two
- * calls at once.  T == 0 is a no-op. */
+ * largest multiple of an e4m3 value that half precision holds, are rounded to it.  A page must not be appended to by two
+ * calls at once, nor by two sequences of one (cs_kv_pages_fork gives each its own).  T == 0 is a no-op. */
 int cs_kv8_append(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch,
                   const void* k_new, const void* v_new, void* stream);
 int cs_kv8_append_f16(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch,
@@ -390,7 +392,8 @@ int cs_kv8_append_f16(const cs_kv8_pool* pool, int32_t layer, const cs_batch* ba
 /* cs_paged_attention_mixed over an 8-bit pool: K_s and V_s are code * scale, read through block_tables[s] and
  * widened to the type of q and out (bf16; fp16 in the _f16 call) without rounding.  (Half precision: a value under 2^-14
  * keeps what half precision has for it, and a scale whose codes pass 61440 is not one that cs_kv8_append_f16 makes.)
- * Everything else is as there.  workspace: at least cs_paged_attention_kv8_workspace_bytes(). */
+ * A row that sees a K or V, or has a Q, that is no number is none; other rows are not touched by it.  Everything else is as there
+ * (cs_set_decode_pages_ahead has no say: 8-bit decode has one depth).  workspace: at least cs_paged_attention_kv8_workspace_bytes(). */
 size_t cs_paged_attention_kv8_workspace_bytes(const cs_batch* batch, int32_t num_q_heads,
                                               int32_t num_kv_heads, int32_t head_dim);
 int cs_paged_attention_mixed_kv8(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch,
@@ -424,7 +427,8 @@ int cs_kv_pages_copy(const cs_page_space* src, int32_t src_layer, const int32_t*
                      int32_t num_layers, int32_t n, void* stream);
 
 /* The block tables of the sequences that share a pool, with their lengths and, for each page, how many
- * table entries hold it (0: free).  All of it lives on the device and is the caller's; row r holds its sequence's pages in
+ * table entries hold it (0: free).  All of it lives on the device and is the caller's, and calls that change the same tables
+ * follow one another (one stream, or events between them); row r holds its sequence's pages in
  * its first ceil(lens[r] / page_size) entries.  A length beyond the row's entries counts as what they hold. */
 typedef struct {
     int32_t* block_tables;          /* device [num_rows][max_blocks_per_seq]             */
@@ -440,7 +444,8 @@ typedef struct {
  * Its first floor(len / page_size) pages are the parent's own (their counts go up by one); an unfinished last page is
  * copied, layers layer_begin .. layer_end - 1, to page fresh_pages[i], whose count becomes 1, so that either may go on
  * appending.  A parent whose length is a multiple of page_size needs none: fresh_pages[i] is not touched then.  The
- * child's other entries become -1; what its row held before is NOT released (cs_kv_pages_free).
+ * child's other entries become -1; what its row held before is NOT released (cs_kv_pages_free).  A fork is one call: a
+ * second one for more layers would count the pages again (cs_kv_pages_copy takes a page's other layers along).
  * parents, children, fresh_pages: device [n].  A parent may be named more often; children must be distinct and no
  * parents, fresh pages distinct and free.  A fork with a row outside the tables is skipped; one that needs a fresh
  * page and has none inside the pool makes a child of the full pages alone. */

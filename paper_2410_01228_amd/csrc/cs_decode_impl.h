@@ -334,6 +334,11 @@ __device__ __forceinline__ void leave_item(
             O += sh_o[w][head][d] * f;
         }
         const int32_t hq = g * G + head;
+        if (E::kEightBit && L != L) {                                 // a score that is no number: nor is the row (pieces: whatever the merge weighs it with)
+            M = 0.f;
+            L = 1.f;
+            O = __builtin_nanf("");
+        }
         if (it.n_splits == 1) {
             const float r = L > 0.f ? O / L : 0.f;                    // no key at all (every page id bad): zeros
             out[((int64_t)t * Hq + hq) * D + d] = (uint16_t)(E::pack(r, 0.f) & 0xffffu);

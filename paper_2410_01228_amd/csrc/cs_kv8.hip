@@ -23,7 +23,7 @@ constexpr float kMostHalf = 61440.f;         // the largest value of 4 significa
 // Where the blocks' scales begin in a page, in bytes.
 __host__ __device__ inline int32_t scales_offset(int32_t Hkv, int32_t D) { return 2 * Hkv * (kPage * D); }
 
-// The new rows' element type.  kMost: a block whose largest value is beyond it is a rare one (rare_top, rare_code): bf16
+// The new rows' element type.  kMost: a block whose largest value is beyond it is a rare one (rare_size, rare_limit): bf16
 // infinities, which end at the largest code and say nothing about the scale; fp16 values beyond kMostHalf, which end there.
 struct RowBf16 {
     static constexpr float kMost = 3.4e38f;
@@ -148,7 +148,7 @@ __device__ __forceinline__ void append8_page(
     if (own.q_len <= 1) return;                                    // single tokens: append8_token
     const int32_t blk = (first >> 4) + (slot_id - ((own.token >> kAppend8SlotShift) + 2 * own.seq));
     const int32_t p0 = blk << 4;
-    if (p0 >= last || blk >= max_blocks) return;
+    if (first < 0 || p0 >= last || blk >= max_blocks) return;
     const bool is_v = threadIdx.x >= 64;
     const int32_t lane = threadIdx.x & 63, tok = lane & 15;
     const int32_t page = block_tables[(int64_t)own.seq * max_blocks + blk];

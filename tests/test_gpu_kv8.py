@@ -309,6 +309,33 @@ def test_a_nan_key_stays_with_the_rows_that_see_it():
     assert torch.isfinite(out[:21]).all() and torch.isnan(out[21:]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("split", [0, 64])
+def test_what_is_no_number_stays_with_the_rows_that_see_it(split, D, dtype):
+    """K, V and Q, in whole and cut decodes, whole and cut chunks: K spoils a kv head's rows, V a feature of them, Q its own row."""
+    Hkv, G = 2, 3
+    w = filled([3000, 500, 0, 1700, 900, 20], [1, 1, 70, 40, 1, 1], Hkv, D, 32, dtype)
+    want = np.zeros((w.T, Hkv * G, D), bool)
+    for s, token, g, kv, d in [(0, 1234, 1, 0, 7), (1, 500, 0, 1, D - 1), (2, 33, 0, 0, 20), (2, 50, 1, 1, 33), (3, 1100, 0, 1, 3), (3, 1739, 1, 0, 0), (5, 3, 0, 0, 1)]:
+        codes, _ = kv8.block(w.pool, 0, int(w.tables[s, token // 16]), kv, g, Hkv, D)
+        codes[(kv8.v_index if kv else kv8.k_index)(token % 16, np.arange(d, d + 1))] = NAN_CODE
+        t0 = int(w.cu[s])
+        for i in range(w.new[s]):
+            if token <= w.ctx[s] + i:
+                want[t0 + i, g * G:(g + 1) * G, d if kv else slice(None)] = True
+    q = queries(w, G)
+    for s, i, h, x in [(4, 0, 2, np.nan), (4, 0, 4, np.inf), (2, 9, 1, -np.inf), (3, 8, 5, np.nan)]:
+        q[int(w.cu[s]) + i, h, D // 2] = x
+        want[int(w.cu[s]) + i, h] = True
+    try:
+        cs.cs_set_decode_split_tokens(split)
+        out = attend(w, G, q)
+    finally:
+        cs.cs_set_decode_split_tokens(0)
+    assert np.array_equal(torch.isnan(out).cpu().numpy(), want) and not torch.isinf(out).any()
+
+
 def test_rows_behind_the_last_sequence_and_outside_the_batch_are_left():
     w = filled([20, 40, 8], [1, 5, 0], 2, 64, 30)
     q = queries(w, 2)
