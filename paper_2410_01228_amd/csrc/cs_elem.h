@@ -103,22 +103,23 @@ struct F16 {
 template <class E> struct Kv8 : E {
     typedef E Wide;
     static constexpr bool kEightBit = true;
-    static constexpr int kCodes = E::kInfinity == 0x7f80u ? 2 : 3;     // that hold a value of Q (QCodes)
+    static constexpr int kCodes = E::kInfinity == 0x7f80u ? 2 : 1;     // of a value of Q in prefill (QCodes), or 1: K is widened there
 };
 
 // Q as codes, for products with K's codes on the 8-bit matrix instruction (a tile of 16 x 16, 128 values of the contraction, with a scale
 // of 2^e for each row and column).  A row of Q is scaled by a power of two to at most 448 and split: its nearest code,
 // 16 times what is left of it as a code, and so on.  A code has 4 significant bits and a rest at most half a step of
-// the code before, so two codes hold a bf16 (8 bits) and three a half (11) without rounding, as far as they are
-// above 2^-18 (2^-22) of the row's largest: fp32 sums round more.  The scales put the parts back in their places.  Two parts take
-// as long as the bf16 product of widened codes, without the widening and with half the bytes to read.
+// the code before, so two codes hold a bf16 (8 bits) without rounding, as far as it is
+// above 2^-18 of the row's largest: fp32 sums round more.  The scales put the parts back in their places.  Two parts take
+// as long as the bf16 product of widened codes, without the widening and with half the bytes to read.  (A half has 11 bits: three
+// codes, half as long again, and more registers than there are; there K is widened.  1024 tokens on 30720 keys, 64/8 heads, fp16: three
+// codes 1016 us, K widened 924; 8 chunks of 2000-2600 on up to 4096, 32/8, 755 and 701.)
 // Lane (column head or query = lane%16, group = lane/16) holds features 16*group .. +16 in the operand's lower half, 64 further on in the
 // upper one; at head dim 64 the upper half is the next part, over the same codes of K.
 typedef int32_t e_i32x8 __attribute__((ext_vector_type(8)));
 template <int D, class E>
 struct QCodes {
-    static constexpr int kParts = E::kCodes;
-    static constexpr int kProducts = D == 128 ? kParts : (kParts + 1) / 2;
+    static constexpr int kParts = 2, kProducts = D == 128 ? kParts : 1;
     e_u32x4 w[kProducts][2];
     uint32_t scale;                                    // byte p: of product p, exponent + 127
 
@@ -147,27 +148,25 @@ struct QCodes {
 #pragma unroll
         for (int i = 0; i < kUnits * 16; ++i) x[i] = __builtin_fmaf(x[i], inv, x[i] - x[i]);   // (an infinity becomes NaN: its scores are none either)
         const uint32_t e0 = (uint32_t)(e + 127);
-        if (D == 128) scale = e0 | (e0 - 4) << 8 | (e0 - 8) << 16;
-        else { const uint32_t p = lane < 32 ? e0 : e0 - 4; scale = p | (p - 8) << 8; }   // of either half: lanes of groups 0-1, 2-3
+        if (D == 128) scale = e0 | (e0 - 4) << 8;
+        else scale = lane < 32 ? e0 : e0 - 4;          // of either half: lanes of groups 0-1, 2-3
 #pragma unroll
-        for (int p = 0; p < 2 * kProducts && (D == 64 || p < kProducts); ++p) {
+        for (int p = 0; p < kParts; ++p) {
 #pragma unroll
             for (int u = 0; u < kUnits; ++u) {
-                e_u32x4 c = {0u, 0u, 0u, 0u};
-                if (p < kParts) {
+                e_u32x4 c;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float* y = x + u * 16 + 4 * i;
-                        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-                        const int both = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
-                        c[i] = (uint32_t)both;
-                        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(both, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(both, true);
-                        y[0] = (y[0] - a[0]) * 16.f; y[1] = (y[1] - a[1]) * 16.f;
-                        y[2] = (y[2] - b[0]) * 16.f; y[3] = (y[3] - b[1]) * 16.f;
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    float* y = x + u * 16 + 4 * i;
+                    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+                    const int both = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+                    c[i] = (uint32_t)both;
+                    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(both, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(both, true);
+                    y[0] = (y[0] - a[0]) * 16.f; y[1] = (y[1] - a[1]) * 16.f;
+                    y[2] = (y[2] - b[0]) * 16.f; y[3] = (y[3] - b[1]) * 16.f;
                 }
                 if (D == 128) w[p][u] = c;
-                else w[p >> 1][p & 1] = c;
+                else w[0][p] = c;
             }
         }
     }
@@ -178,8 +177,6 @@ struct QCodes {
         acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, join(w[0][0], w[0][1]), acc, 0, 0, 0, (int)k_scale, 0, (int)scale);
         if constexpr (kProducts > 1)
             acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, join(w[1][0], w[1][1]), acc, 0, 0, 0, (int)k_scale, 1, (int)scale);
-        if constexpr (kProducts > 2)
-            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, join(w[2][0], w[2][1]), acc, 0, 0, 0, (int)k_scale, 2, (int)scale);
         return acc;
     }
 

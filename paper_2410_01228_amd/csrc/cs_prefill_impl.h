@@ -152,22 +152,23 @@ struct PrefillLds {
 // From an 8-bit pool: the codes of the next steps -- K as operands, V as the lanes' own 16-byte units, where they find them again
 // -- and the scales of 64 pages (two windows of them) for each wavefront; V once more, widened.
 constexpr int kAhead8 = 2;                            // steps on their way beyond the one that the next iteration needs
-constexpr int kRing8V = 2;
-// Three codes a value of Q are more registers than there are: the last ones wait in LDS (spilled by the compiler they come
-// back as memory loads, each of which waits for all copies under way: 1024 tokens on 30720 keys, 64/8 heads, 1020 us with them in
-// LDS, 1127 spilled; with those of one of the two column tiles in LDS the rest still spills, 1226).
-template <int D, int kCodes> constexpr bool kQInLds = kCodes == 3 && D == 128;
+constexpr int kWide8 = 2;                             // steps of which widened codes are kept
 template <int D>
 struct PrefillLds8 {
     u32x4 k[kRing][2 * D];
     u32x4 v_codes[kRing][2 * D];
-    u32x4 v[kRing8V][4 * D];
+    u32x4 v[kWide8][4 * D];
     float scale[2][kPrefillWaves][2][64];             // [window][wavefront][K, V][page]
     int32_t last;
 };
 template <int D> struct PrefillLds<D, 2> : PrefillLds8<D> {};
-template <int D> struct PrefillLds<D, 3> : PrefillLds8<D> {
-    u32x4 q_low[kQInLds<D, 3> ? kPrefillWaves : 1][kNCT][2][64];
+template <int D> struct PrefillLds<D, 1> {            // K like V
+    u32x4 k_codes[kRing][2 * D];
+    u32x4 v_codes[kRing][2 * D];
+    u32x4 k[kWide8][4 * D];
+    u32x4 v[kWide8][4 * D];
+    float scale[2][kPrefillWaves][2][64];
+    int32_t last;
 };
 static_assert(kAhead8 + 2 <= kRing, "K of the steps i+1 .. i+2+kAhead8");
 
@@ -210,7 +211,8 @@ __device__ __forceinline__ void prefill_tile(
     constexpr int kStepLoads = (kLaneAddr ? 2 : 2 * kStepPages) * kLoads;   // LDS-DMA instructions per wavefront and step
     constexpr int kPartRow = D + 4;                   // floats per query row of a partial: D outputs, max, sum, pad
     constexpr bool kEight = E::kEightBit;
-    constexpr int kSlotsV = kEight ? kRing8V : kRing;
+    constexpr bool kWidenK = E::kCodes == 1, kQCodes = kEight && !kWidenK;
+    constexpr int kSlotsV = kEight ? kWide8 : kRing, kSlotsK = kWidenK ? kWide8 : kRing;
     static_assert(!kEight || PS == 16, "8-bit pools have pages of 16 tokens");
     auto& lds_k = lds.k;
     auto& lds_v = lds.v;
@@ -244,11 +246,10 @@ __device__ __forceinline__ void prefill_tile(
     // kFold (element types that stand it, see cs_elem.h): Q is scaled once by scale*log2(e), so the
     // matrix unit delivers the scores in the exponent's domain, and the score accumulators start
     // from minus the running offset, so exp2 takes them as they come -- no multiply-add per score.
-    // (not with 8-bit codes: three of them hold a half exactly, and the accumulators' start takes registers that are short)
-    constexpr bool kFold = E::kScaleFoldsIntoQ && !kEight;
+    constexpr bool kFold = E::kScaleFoldsIntoQ && !kQCodes;
     // ---- this wavefront's column tiles: ct = wave*4 + c -> (token block, head) ----
-    u32x4 qb[kEight ? 1 : kNCT][D / 32];
-    QCodes<D, E> q8[kEight ? kNCT : 1];                // 8-bit pools: Q in codes too
+    u32x4 qb[kQCodes ? 1 : kNCT][D / 32];
+    QCodes<D, E> q8[kQCodes ? kNCT : 1];               // 8-bit pools: Q in codes too
     int32_t pos_q[kNCT];                               // absolute position of this lane's query
     const u32x4 zero4 = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -258,12 +259,8 @@ __device__ __forceinline__ void prefill_tile(
         const int32_t tl = tb * 16 + (lane & 15);            // chunk-local token of this column
         const bool valid = ct < n_ct && tl < q_len;
         pos_q[c] = C + tl;
-        if constexpr (kEight) {
+        if constexpr (kQCodes) {
             q8[c].load(q + ((int64_t)(t_seq + tl) * Hq + g * G + hh) * D, valid, lane);
-            if constexpr (kQInLds<D, E::kCodes>) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u) lds.q_low[wave][c][u][lane] = q8[c].w[2][u];
-            }
         } else {
 #pragma unroll
             for (int kk = 0; kk < D / 32; ++kk) {
@@ -403,12 +400,14 @@ __device__ __forceinline__ void prefill_tile(
         }
     };
 
-    // ---- 8-bit pools.  K is never widened: its codes are copied to LDS as operands of the 8-bit matrix instruction (one 16-byte
-    // unit, 16 features of a token, is half a lane's operand), Q is split into codes (QCodes), and the instruction
-    // applies the blocks' scales.  V is copied as it is, a unit a lane; the lane that copied it reads it back an iteration later, widens
+    // ---- 8-bit pools.  Under a bf16 Q, K is never widened: its codes are copied to LDS as operands of the 8-bit matrix instruction (one
+    // 16-byte unit, 16 features of a token, is half a lane's operand), Q is split into codes (QCodes), and the instruction
+    // applies the blocks' scales.  V, and K under an fp16 Q, is copied as it is, a unit a lane; the lane that copied it reads it back an iteration later, widens
     // it and writes it in the arrangement above -- once a workgroup, because widened by every wavefront as it reads
     // its operands a step would cost each 32 conversions; the weights, unlike Q, are new every step, and splitting them would cost
-    // more than that.  A unit of V is 4 tokens of a feature in each of 4 feature tiles, half a 16-bit unit in each.
+    // more than that.  A unit of V is 4 tokens of a feature in each of 4 feature tiles, half a 16-bit unit in each; one of K is 16
+    // features of a token, two 16-bit units.  K is widened a step before V, in time for the barrier ahead of the reads; so with fp16 all
+    // copies leave a step earlier.
     // Head dim 64: K is copied by the lower two wavefronts, V by the upper two. ----
     constexpr int kLoads8 = D == 64 ? 1 : kLaneAddr ? 2 : 3;                           // LDS-DMA instructions per wavefront and step, at least
     const bool k_wave = D == 128 || wave < 2, v_wave = D == 128 || wave >= 2;
@@ -424,7 +423,9 @@ __device__ __forceinline__ void prefill_tile(
                 load_window();
             }
             const int j = kStepPages * step - idbase;
-            u32x4* const k_to = &lds.k[(uint32_t)step % kRing][unit0_8];
+            u32x4* k_to;
+            if constexpr (kWidenK) k_to = &lds.k_codes[(uint32_t)step % kRing][unit0_8];
+            else k_to = &lds.k[(uint32_t)step % kRing][unit0_8];
             u32x4* const v_to = &lds.v_codes[(uint32_t)step % kRing][unit0_8];
             if constexpr (kLaneAddr) {
                 auto unit = [&](u32x4* dst, int page, uint32_t off) {
@@ -466,6 +467,21 @@ __device__ __forceinline__ void prefill_tile(
         }
     };
 
+    auto widen8_k = [&](int32_t step) {
+        if constexpr (kWidenK) {
+            if (k_wave) {
+                const u32x4 w = lds.k_codes[(uint32_t)step % kRing][unit0_8 + lane];
+                const float f = scale8(step, 0, k_row >> 3);
+                const int grp = lane >> 4;
+                u32x4* to = &lds_k[(uint32_t)step % kSlotsK][((k_u * 2 + (grp >> 1)) * 2 + k_tile) * 64 + (grp & 1) * 32 + k_row];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    to[h * 16] = u32x4{E::template widen<false>(w[2 * h], f), E::template widen<true>(w[2 * h], f),
+                                       E::template widen<false>(w[2 * h + 1], f), E::template widen<true>(w[2 * h + 1], f)};
+            }
+        }
+    };
+
     // Raw scores of one step (before the softmax scale).  With hi = lane/16: xs[c][0..3] are
     // rows 4*hi + i of tile X, xs[c][4..7] of tile Y, i.e. together the 8 consecutive keys
     // 32*step + 16*(hi/2) + 8*(hi%2) + 0..7.  Masked entries become -inf.
@@ -477,14 +493,14 @@ __device__ __forceinline__ void prefill_tile(
     f32x4 neg_off[kNCT];
 #pragma unroll
     for (int c = 0; c < kNCT; ++c) neg_off[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr int kRegsK = kEight ? 2 * (D / 64) : 2 * (D / 32);
+    constexpr int kRegsK = kQCodes ? 2 * (D / 64) : 2 * (D / 32);
     u32x4 kreg[kRegsK];
     uint32_t k_scale = 0;                              // 8-bit: exponent of the block of this lane's row, in both tiles
     auto load_k = [&](int32_t step) {
-        const u32x4* kA = &lds_k[(uint32_t)step % kRing][0];
+        const u32x4* kA = &lds_k[(uint32_t)step % kSlotsK][0];
 #pragma unroll
         for (int u = 0; u < kRegsK; ++u) kreg[u] = kA[u * 64 + lane];          // (kk*2 + tile)
-        if constexpr (kEight) k_scale = __builtin_bit_cast(uint32_t, scale8(step, 0, k_row >> 3)) >> 23;
+        if constexpr (kQCodes) k_scale = __builtin_bit_cast(uint32_t, scale8(step, 0, k_row >> 3)) >> 23;
     };
     auto scores = [&](auto masked, int32_t step, float (&xs)[kNCT][8]) {
         constexpr bool kMask = decltype(masked)::value;
@@ -494,13 +510,9 @@ __device__ __forceinline__ void prefill_tile(
             if constexpr (kFold) { s0[c] = neg_off[c]; s1[c] = neg_off[c]; }
             else { s0[c] = f32x4{0.f, 0.f, 0.f, 0.f}; s1[c] = f32x4{0.f, 0.f, 0.f, 0.f}; }
         }
-        if constexpr (kEight) {
+        if constexpr (kQCodes) {
 #pragma unroll
             for (int c = 0; c < kNCT; ++c) {
-                if constexpr (kQInLds<D, E::kCodes>) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) q8[c].w[2][u] = lds.q_low[wave][c][u][lane];
-                }
                 s0[c] = q8[c].dot(kreg[0], kreg[kRegsK - 2], k_scale, s0[c]);    // tile X
                 s1[c] = q8[c].dot(kreg[1], kreg[kRegsK - 1], k_scale, s1[c]);    // tile Y
             }
@@ -581,7 +593,25 @@ __device__ __forceinline__ void prefill_tile(
     // ---- prologue: the first kRing-1 steps of the range in flight, the first two landed,
     // scores of the first step, K operands of the second ----
     StepPages pg_next;                                            // pages of the step issued next
-    if constexpr (kEight) {
+    if constexpr (kWidenK) {
+#pragma unroll
+        for (int j = 0; j < kAhead8 + 2; ++j) copy8(step_begin + j);
+        wait_vmcnt<(kAhead8 - 1) * kLoads8>();                    // (copies that the lane itself made)
+        __builtin_amdgcn_sched_barrier(0);
+        widen8_k(step_begin);
+        widen8_k(step_begin + 1);
+        widen8(step_begin);
+        widen8(step_begin + 1);
+        __syncthreads();
+        load_k(step_begin);
+        scores(std::true_type{}, step_begin, x);
+        raise_max(x);
+        load_k(step_begin + 1);
+        __syncthreads();                                          // every wavefront has read both
+        widen8_k(step_begin + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        copy8(step_begin + kAhead8 + 2);
+    } else if constexpr (kEight) {
 #pragma unroll
         for (int j = 0; j < kAhead8 + 2; ++j) copy8(step_begin + j);
         wait_vmcnt<kAhead8 * kLoads8>();
@@ -613,8 +643,8 @@ __device__ __forceinline__ void prefill_tile(
     // i+2 are fetched and the new scores are tested against the running maxima.
     // kMask: causal / end-of-sequence masking (needed from the first edge step on);
     // kLast: there is no step i+1. ----
-    // From an 8-bit pool, iteration i sends for step i+2+kAhead8, and its second half also widens V(i+2) into the slot that V(i)
-    // left before the barrier.
+    // From an 8-bit pool, iteration i sends for step i+2+kAhead8 (fp16: one later), and its second half also widens V(i+2) into the
+    // slot that V(i) left before the barrier, and for an fp16 Q K(i+3) into that of K(i+1).
     bool saw_nan = false;
     auto iteration = [&](auto masked, auto last, int32_t i, float (&xc)[kNCT][8], float (&xn)[kNCT][8]) {
         constexpr bool kMask = decltype(masked)::value;
@@ -630,7 +660,7 @@ __device__ __forceinline__ void prefill_tile(
             dma_step(i + kRing - 1, pg_next);
             pg_next = step_pages(i + kRing);           // consumed by the next iteration
         } else if (!kLast) {
-            copy8(i + 2 + kAhead8);
+            copy8(i + 2 + kAhead8 + kWidenK);
         }
 
         if (!kLast) scores(masked, i + 1, xn);
@@ -687,7 +717,7 @@ __device__ __forceinline__ void prefill_tile(
             // steady state, first half: tell the scheduler the order we want.  The exp / convert
             // work of step i runs under the score MFMAs of step i+1, and the V operands are
             // fetched under them too.
-            constexpr int kQK = 2 * kNCT * (kEight ? QCodes<D, E>::kProducts : D / 32);
+            constexpr int kQK = 2 * kNCT * (kQCodes ? QCodes<D, E>::kProducts : D / 32);
             __builtin_amdgcn_sched_group_barrier(0x002, 4 * kNCT, 0);            // VALU
 #pragma unroll
             for (int r = 0; r < kQK; ++r) {
@@ -706,7 +736,10 @@ __device__ __forceinline__ void prefill_tile(
 
         if (kPriority) __builtin_amdgcn_s_setprio(kPriority);
         if (!kLast) load_k(i + 2);
-        if constexpr (kEight && !kLast) widen8(i + 2);
+        if constexpr (kEight && !kLast) {
+            widen8(i + 2);
+            widen8_k(i + 3);
+        }
 #pragma unroll
         for (int c = 0; c < kNCT; ++c)
             lacc[c] = E::mfma32(ones, pb[c], lacc[c]);
@@ -722,10 +755,10 @@ __device__ __forceinline__ void prefill_tile(
             constexpr int kPV = kNCT + kNCT * (D / 16);
 #pragma unroll
             for (int r = 0; r < kPV; ++r) {
-                if (kEight && r == 0) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);                 // the codes and the scale to widen
+                if (kEight && r == 0) __builtin_amdgcn_sched_group_barrier(0x100, kWidenK ? 4 : 2, 0);                 // the codes and the scale to widen
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x002, kEight ? 2 : 1, 0);
-                if (r >= 2 && r < 2 + kRegsK + kEight) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // K: one ds_read_b128
+                if (r >= 2 && r < 2 + kRegsK + kQCodes) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // K: one ds_read_b128
                 if (kEight && r >= kPV - 2) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);           // what has been widened
             }
         }
