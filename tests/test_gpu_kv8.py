@@ -424,3 +424,71 @@ def test_synth_batches_run_in_both_caches():
     w = filled(ctx, new, b.shape.Hkv, b.shape.D, 34)
     q = queries(w, b.shape.G)
     check_attention(w, b.shape.G, attend(w, b.shape.G, q), q)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("ctx,new", [([5000, 16], [40, 700]), ([4200], [600])])
+def test_chunks_over_many_windows_of_pages(ctx, new, D, dtype):
+    w = filled(ctx, new, 1, D, 33, dtype)
+    q = queries(w, 4)
+    check_attention(w, 4, attend(w, 4, q), q)
+
+
+def test_two_graphs_share_a_workspace():
+    """One batch with cut decodes and cut chunks in bf16, one in fp16, replayed in turn in one workspace with an eager call between."""
+    runs = []
+    for seed, dtype, ctx, new in ((34, torch.bfloat16, [2900, 30, 1500], [1, 1, 60]), (35, torch.float16, [1, 2600, 4000], [1, 1, 33])):
+        w = filled(ctx, new, 2, 128, seed, dtype)
+        q, b = queries(w, 4), w.batch()
+        pool = w.handle(torch.from_numpy(w.pool).cuda())
+        runs.append((cs.cs_paged_attention_mixed_kv8 if dtype == torch.bfloat16 else cs.cs_paged_attention_mixed_kv8_f16, pool, b, q, torch.empty_like(q)))
+    ws = torch.empty(max(cs.cs_paged_attention_kv8_workspace_bytes(r[2], 8, 2, 128) for r in runs), dtype=torch.uint8, device="cuda")
+    want, graphs = [], []
+    for fn, pool, b, q, out in runs:
+        fn(pool, 0, b, q, out, 8, 0.09, ws)
+        torch.cuda.synchronize()
+        want.append(out.clone())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            fn(pool, 0, b, q, out, 8, 0.09, ws)
+    for i in range(6):
+        for r, g, x in zip(runs, graphs, want):
+            r[4].zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(r[4], x)
+        if i % 2:
+            fn, pool, b, q, out = runs[i // 2 % 2]
+            fn(pool, 0, b, q, out, 8, 0.09, ws)
+            torch.cuda.synchronize()
+
+
+def test_two_threads_on_streams_of_their_own():
+    import threading
+    ws, got, failed = [filled([2000, 30, 700], [1, 1, 50], 2, 128, s) for s in (36, 37)], [None, None], []
+    qs = [queries(w, 4) for w in ws]
+    want = [attend(w, 4, q) for w, q in zip(ws, qs)]
+    torch.cuda.synchronize()
+
+    def work(i):
+        try:
+            w, b, stream = ws[i], ws[i].batch(), torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                pool, space = w.handle(torch.from_numpy(w.pool).cuda()), cs.workspace_for_kv8(b, 8, 2, 128)
+                outs = [torch.empty_like(qs[i]) for _ in range(20)]
+                for out in outs:
+                    cs.cs_paged_attention_mixed_kv8(pool, 0, b, qs[i], out, 8, 1.0 / np.sqrt(128), space, stream)
+            stream.synchronize()
+            got[i] = outs
+        except Exception as e:                                            # (a thread's own failure would go unseen)
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    for x, outs in zip(want, got):
+        assert all(torch.equal(out, x) for out in outs)
