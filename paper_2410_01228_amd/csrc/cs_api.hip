@@ -463,6 +463,92 @@ static void play_pairs(const cs_batch* b, const DecodePlan& d, int32_t Hkv, int3
     *behind = *std::max_element(ends.begin(), ends.end()) * 2 * groups / sum;
 }
 
+// Steps of every tile slot of a plan (0: an empty slot).
+static std::vector<int32_t> steps_of_slots(const cs_batch* b, const PrefillPlan& p, int32_t G) {
+    std::vector<int32_t> slot_steps((size_t)p.num_slots, 0);
+    for (int32_t s = 0; s < b->num_seqs; ++s) {
+        const int32_t ql = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s];
+        if (ql <= 1) continue;
+        const int32_t n_ct = ((ql + 15) >> 4) * G;
+        const int64_t slot0 = prefill_slot_start(b->h_cu_q_lens[s], s, G) - p.base_slot;
+        for (int32_t ct0 = 0; ct0 < n_ct; ct0 += kTileCols) {
+            const int32_t tb_max = (std::min(ct0 + kTileCols, n_ct) - 1) / G;
+            const int32_t n_keys = b->h_ctx_lens[s] + std::min(ql, (tb_max + 1) * 16);
+            slot_steps[(size_t)(slot0 + ct0 / kTileCols)] = (n_keys + kKeysPerStep - 1) / kKeysPerStep;
+        }
+    }
+    return slot_steps;
+}
+
+// 8-bit pools, head dim 128: two kernels (0), behind (1) or beside (2) the tiles, the tiles whole or cut as planned for a grid of
+// their own (p is changed), whichever of the five the model below has fastest; mode 2 or 3: of those with decode behind or
+// beside.  Decode work of half the bytes is rarely what a mix waits for, and the rules for 16 bits, fitted where it often is, miss three
+// things: tiles cut to fill a chip of their own, which decode work would have filled (4 chunks of 512 tokens + 64 decodes, 28/4 heads:
+// 315 us cut, 275 whole); tiles of unequal chunks, which the prefill kernel launches longest first, the fused grid in the batch's
+// order (4 chunks on 230-6500 keys + 10 short decodes, 40/8: 286 and 209 in two kernels); and that a decode workgroup a CU,
+// one step of 32 keys ahead, no longer fills the memory (132 decodes of 350-1400 keys + 5 short chunks, 64/8: 62 beside, 52 behind).
+// Behind and tiles as in plan_fusion_by_model; beside, the decode side takes 1.15 of its time; then in microseconds what the calls
+// measured take on top: 13 behind, 16 beside, two kernels 24, the join of cut tiles 3 and their partials at 5 TB/s.  Over 190 drawn
+// mixes (8-256 decodes of 100-24000 keys, 1-5 chunks of 32-3700 tokens, four model shapes) off the best of the five: this 0.6% on average, 19%
+// at worst; the 16-bit rules, over 90 of them, 3.2% and 39%; always behind 2.1% and 39%.
+static int32_t arrange8(const cs_batch* b, const DecodePlan& d, PrefillPlan& p, int32_t Hkv, int32_t G, int32_t D, int32_t mode) {
+    const int32_t groups = std::max(1, device_cus() / Hkv);
+    const double us_per_step = 0.88, t_dec = (double)d.decode_keys * 2 * Hkv * D / 6.5e6;
+    const std::vector<int32_t> slot_steps = steps_of_slots(b, p, G);
+    const int32_t longest = std::max(1, *std::max_element(slot_steps.begin(), slot_steps.end()));
+    std::vector<float> work;
+    auto list_work = [&](int32_t range_steps, int32_t ranges) {
+        work.clear();
+        for (int32_t r = 0; r < ranges; ++r)
+            for (int32_t pos = 0; pos < p.num_slots; ++pos) {
+                const int32_t n = std::min(slot_steps[(size_t)(p.backwards ? p.num_slots - 1 - pos : pos)], (r + 1) * range_steps) - r * range_steps;
+                if (n > 0) work.push_back((float)((n + 8) * us_per_step));
+            }
+    };
+    std::vector<double> free_at;
+    auto behind = [&] {
+        play_tiles(work, groups, 0.0, free_at);
+        std::sort(free_at.begin(), free_at.end());
+        double t = 0, left = t_dec;
+        const double sat = 1.56 * groups;
+        for (size_t i = 0; ; ++i) {
+            const double rate = std::min(1.0, (double)i / sat);                  // i slots (of every CU of a group) are free
+            const double next = i < free_at.size() ? free_at[i] : 1.0e300;
+            if (rate > 0 && t + left / rate <= next) return std::max(t + left / rate, free_at.back()) + 13.0;
+            left -= rate * (next - t);
+            t = next;
+        }
+    };
+    auto beside = [&] { return std::max(play_tiles(work, groups, 1.15 * t_dec, free_at), 1.15 * t_dec) + 16.0; };
+    double best = 1.0e300;
+    int32_t arrangement = 1;
+    bool whole = false;
+    auto take = [&](double t, int32_t a, bool w) {
+        if (t < best) { best = t; arrangement = a; whole = w; }
+    };
+    const double join = p.max_ranges > 1 ? 3.0 + (double)p.num_slots * Hkv * p.max_ranges * kTileCols * 16 * (D + 4) * 4.0 / 5.0e6 : 0.0;
+    list_work(p.range_steps, p.max_ranges);
+    if (mode != 3) take(behind() + join, 1, false);
+    if (mode != 2) take(beside() + join, 2, false);
+    if (mode == 1) {
+        if (p.n_ordered > 0) std::stable_sort(work.begin(), work.end(), std::greater<float>());
+        take(play_tiles(work, groups, 0.0, free_at) + t_dec + join + 24.0, 0, false);
+    }
+    if (p.max_ranges > 1) {
+        list_work(longest, 1);
+        if (mode != 3) take(behind(), 1, true);
+        if (mode != 2) take(beside(), 2, true);
+    }
+    if (whole) {
+        p.n_ordered = 0;
+        p.cut_first_pos = p.num_slots;
+        p.range_steps = longest;
+        p.max_ranges = 1;
+        p.bytes = 0;
+    }
+    return arrangement;
+}
+
 // The choice between "behind" and "beside" comes from playing both grids (play_tiles).  A tile
 // workgroup of n steps takes (n + 8) * 0.88 us (a 32-key step at head dim 128 beside another
 // tile).  Behind: the decode bytes flow at 6.5 TB/s times min(1, free slots / (1.56 CUs)) into
@@ -499,6 +585,12 @@ static FusePlan plan_fusion_by_model(const cs_batch* b, const DecodePlan& d, Pre
     f.arrangement = 1;
     f.prio = t_decode < 0.3 * t_prefill ? 1 : 0;
     const int32_t cus = device_cus();
+    if (d.elem_bytes == 1 && D == 128 && (int64_t)p.num_slots * p.max_ranges <= 8192) {
+        const int32_t a = arrange8(b, d, p, Hkv, G, D, mode);
+        if (a == 0) return FusePlan{0, 0, 0};
+        if (a == 1) return f;
+        mode = 3;
+    }
     // (head dim 64 fits three workgroups per CU, both kinds already share CUs behind the tiles,
     // and beside wins on some mixes and loses on others: the choice there is not modelled)
     if (mode == 2 || (mode == 1 && D != 128)) return f;
@@ -537,18 +629,7 @@ static FusePlan plan_fusion_by_model(const cs_batch* b, const DecodePlan& d, Pre
             beside = beside || t_decode >= 0.5 * t_prefill;
         } else {
             // steps of every tile slot, then the workgroups in the fused grid's launch order
-            std::vector<int32_t> slot_steps((size_t)p.num_slots, 0);
-            for (int32_t s = 0; s < b->num_seqs; ++s) {
-                const int32_t ql = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s];
-                if (ql <= 1) continue;
-                const int32_t n_ct = ((ql + 15) >> 4) * G;
-                const int64_t slot0 = prefill_slot_start(b->h_cu_q_lens[s], s, G) - p.base_slot;
-                for (int32_t ct0 = 0; ct0 < n_ct; ct0 += kTileCols) {
-                    const int32_t tb_max = (std::min(ct0 + kTileCols, n_ct) - 1) / G;
-                    const int32_t n_keys = b->h_ctx_lens[s] + std::min(ql, (tb_max + 1) * 16);
-                    slot_steps[(size_t)(slot0 + ct0 / kTileCols)] = (n_keys + kKeysPerStep - 1) / kKeysPerStep;
-                }
-            }
+            const std::vector<int32_t> slot_steps = steps_of_slots(b, p, G);
             auto steps_at = [&](int32_t pos) { return slot_steps[(size_t)(p.backwards ? p.num_slots - 1 - pos : pos)]; };
             // the grid's tile workgroups in launch order: whole tiles up to position `whole`, then,
             // range-major, the ranges of `range_steps` steps of the tiles behind them

@@ -182,3 +182,27 @@ def test_spaces_of_pools():
     assert (s.page_bytes, s.layer_stride, s.page_stride) == (4112, 8 * 4224, 4224)
     assert cs.lib().cs_kv8_page_space(ctypes.byref(p8), None) == cs.CS_ERR_INVALID_ARG
     assert cs.lib().cs_kv_page_space(ctypes.byref(p16), None) == cs.CS_ERR_INVALID_ARG
+
+
+def host_batch(ctx, new):
+    blocks = max(-(-(c + n) // 16) for c, n in zip(ctx, new))
+    return cs.Batch(torch.zeros((len(ctx), max(blocks, 1)), dtype=torch.int32), torch.tensor(ctx, dtype=torch.int32),
+                    torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), device="cpu")
+
+
+def test_attention_plans_of_drawn_batches():
+    """The plan, and with it the workspace, is a function of the batch: the same when other batches were planned between."""
+    r = np.random.default_rng(4)
+    drawn = []
+    for _ in range(60):
+        hq, hkv, d = [(32, 8, 128), (28, 4, 128), (64, 8, 128), (40, 8, 128), (4, 2, 64), (6, 6, 64)][r.integers(6)]
+        n = int(r.integers(1, 40))
+        ctx = (10 ** r.uniform(0, 4.3, n)).astype(int).tolist()
+        new = np.where(r.random(n) < 0.8, 1, r.integers(0, 900, n)).tolist()
+        drawn.append((ctx, new, hq, hkv, d))
+    first = [cs.cs_paged_attention_kv8_workspace_bytes(host_batch(c, n), hq, hkv, d) for c, n, hq, hkv, d in drawn]
+    for (c, n, hq, hkv, d), x in reversed(list(zip(drawn, first))):
+        b = host_batch(c, n)
+        assert cs.cs_paged_attention_kv8_workspace_bytes(b, hq, hkv, d) == x < 1 << 31
+        cs.cs_paged_attention_workspace_bytes(b, hq, hkv, d)                        # (the 16-bit plan of the same lengths is another)
+        assert cs.cs_paged_attention_kv8_workspace_bytes(b, hq, hkv, d) == x
