@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kPlanThreads) void decode_plan_kernel(
 }
 
 // grid = (items * Hkv, layers) workgroups, kv head fastest (the heads of one page are neighbours
-// in memory, so neighbouring workgroups share DRAM pages and translations).
+// in memory, so neighbouring workgroups share DRAM pages and translations); 8-bit pools: pair_of8.
 // kCut: a list in the arguments that holds pieces, which part.words may ask to merge in place.  (Launches
 // without cuts run pages of 8 tokens 4% faster without that code: 137 sequences of 47-349 keys, 64/8 heads,
 // 27.0 -> 26.1 us.  Cut lists that a kernel merges are faster with it: 64 of 1K-8K keys, 28/4 heads, the
@@ -66,7 +66,9 @@ __device__ __forceinline__ void split_workgroup(
     float scale_log2e, const DecodePartials& part, int64_t next_layer, int64_t next_q)
 {
     __shared__ DecodeLds<D> lds;
-    const int32_t item = blockIdx.x / Hkv, g = blockIdx.x - item * Hkv, n_items = gridDim.x / Hkv;
+    const int32_t n_items = gridDim.x / Hkv;
+    int32_t item = blockIdx.x / Hkv, g = blockIdx.x - item * Hkv;
+    if constexpr (E::kEightBit) pair_of8(blockIdx.x, Hkv, n_items, item, g);
     const DecodePartials mine = part.of_layer(blockIdx.y, n_items, Hkv * G, Hkv, D);
     out += blockIdx.y * next_q;
     if constexpr (E::kEightBit)

@@ -120,11 +120,27 @@ __device__ __forceinline__ void process_step8(WaveState<D>& st, const StepRegs8<
         }
 }
 
+// The (item, kv head) of pair w of a grid: eight items at a time, their heads in turn, so that the heads of an item go to one XCD
+// (workgroups are dealt round-robin to the 8 of them; fewer than eight items that are left over: head by head).  A page's scales are one
+// cache line for all heads: with the heads of a page spread over the XCDs each L2 fetches it, 64 bytes of use to a head's 4 KiB (256
+// decodes of 512-4096 keys, 32/8 heads, 199.6 -> 186.7 us, 6.71 TB/s; 64 of 4096, 96.0 -> 81.0; 32 of 300-3000, 30.3 -> 22.2; 300 of 50-500,
+// 64/8, 38.2 -> 33.5; 64 of 1000-8000, 28/4, 58.7 -> 56.9).
+__device__ __forceinline__ void pair_of8(int32_t w, int32_t Hkv, int32_t n_items, int32_t& item, int32_t& g) {
+    item = w / Hkv;
+    g = w - item * Hkv;
+    const int32_t first = item & ~7;
+    if (first + 8 <= n_items) {
+        const int32_t r = w - first * Hkv;
+        item = first + (r & 7);
+        g = r >> 3;
+    }
+}
+
 // decode_item for 8-bit pools: page_stride in units of 2 bytes.
 //
 // One form for every launch: a step ahead, with loads that the compiler can count (Loads::kLone there).  A workgroup
 // takes half as long as over 16-bit pages, so more of a launch is the time of its last ones, alone on their CUs, and full chips
-// do not mind: skipped loads, one step ahead, 256 decodes of 512-4096 keys, 32/8 heads, 194.6 us, this 192.3; of 1000-8000, 4/2
+// do not mind (figures from before pair_of8, which took 1-27% off either side): skipped loads, one step ahead, 256 decodes of 512-4096 keys, 32/8 heads, 194.6 us, this 192.3; of 1000-8000, 4/2
 // heads, 90 and 64; 8 of 128-2048 uncut, 32/8, 24.9 and 18.0.  Two steps ahead are within 0.3% on full chips, up to 8% faster for a
 // few long items (1 of 20000, 64/8, pieces of 1024: 18.5 us instead of 19.9) and 1-18% slower for many short ones (300 of
 // 50-500: 48.7 instead of 41.2).  Four workgroups a CU, in 128 registers, spill: 244 us.

@@ -83,9 +83,10 @@ __global__ __launch_bounds__(kPrefillThreads, 2) void mixed_kernel(
         for (uint32_t base = 0, round = 0; base < n_decode; base += dec_wgs, ++round) {
             const uint32_t w = base + ((round & 1) ? dec_wgs - 1 - j : j);
             if (w >= n_decode) continue;
-            int32_t item = w / Hkv;
-            const int32_t g = w - item * Hkv, l = item / n_items;
+            int32_t item = w / Hkv, g = w - item * Hkv;
+            const int32_t l = item / n_items;
             item -= l * n_items;
+            if constexpr (E::kEightBit) pair_of8(w, Hkv, n_items, item, g);        // (one layer)
             const DecodePartials mine = part.of_layer(l, n_items, Hkv * G, Hkv, D);
             // one page ahead, with loads the compiler can count (a workgroup that shares its CU
             // with a tile must stream by itself); a deeper queue only delays the tile's own
