@@ -256,6 +256,7 @@ class Pool8:
         self.page_bytes = cs_kv8_page_bytes(Hkv, D)
         self.page_stride = self.page_bytes if page_stride is None else page_stride
         self.layer_stride = P * self.page_stride if layer_stride is None else layer_stride
+        assert tensor.numel() * tensor.element_size() >= (L - 1) * self.layer_stride + P * self.page_stride
         self.c = cs_kv8_pool(_ptr(tensor), L, P, Hkv, D, self.layer_stride, self.page_stride)
         self.L, self.P, self.Hkv, self.D = L, P, Hkv, D
 
@@ -592,6 +593,7 @@ def cs_kv_pages_copy(src: PageSpace, src_layer: int, src_ids: Optional[torch.Ten
     """n: by default the length of the id lists; needed where both are None."""
     if n is None:
         n = (src_ids if src_ids is not None else dst_ids).numel()
+    assert all(t is None or (t.dtype == torch.int32 and t.numel() >= n) for t in (src_ids, dst_ids))
     _check(lib().cs_kv_pages_copy(ctypes.byref(src.c), src_layer, _ptr(src_ids), ctypes.byref(dst.c), dst_layer, _ptr(dst_ids),
                                   num_layers, n, _stream(stream)), "cs_kv_pages_copy")
 
@@ -599,19 +601,22 @@ def cs_kv_pages_copy(src: PageSpace, src_layer: int, src_ids: Optional[torch.Ten
 def cs_kv_pages_fork(space: PageSpace, layer_begin: int, layer_end: int, tables: PageTables, parents: torch.Tensor,
                      children: torch.Tensor, fresh_pages: torch.Tensor, stream=None):
     assert parents.numel() == children.numel() == fresh_pages.numel()
+    assert parents.dtype == children.dtype == fresh_pages.dtype == torch.int32
     _check(lib().cs_kv_pages_fork(ctypes.byref(space.c), layer_begin, layer_end, ctypes.byref(tables.c), _ptr(parents), _ptr(children),
                                   _ptr(fresh_pages), parents.numel(), _stream(stream)), "cs_kv_pages_fork")
 
 
 def cs_kv_pages_free(tables: PageTables, rows: torch.Tensor, freed: torch.Tensor, num_freed: torch.Tensor, stream=None):
-    assert freed.numel() >= tables.ref_counts.numel()
+    assert freed.numel() >= tables.ref_counts.numel() and num_freed.numel() >= 1
+    assert rows.dtype == freed.dtype == num_freed.dtype == torch.int32
     _check(lib().cs_kv_pages_free(ctypes.byref(tables.c), _ptr(rows), rows.numel(), _ptr(freed), _ptr(num_freed), _stream(stream)),
            "cs_kv_pages_free")
 
 
 def cs_kv_pages_compact(space: PageSpace, layer_begin: int, layer_end: int, tables: PageTables, new_tables: PageTables,
                         new_ids: torch.Tensor, num_used: torch.Tensor, workspace: torch.Tensor, stream=None):
-    assert new_ids.numel() >= tables.ref_counts.numel()
+    assert new_ids.numel() >= tables.ref_counts.numel() and num_used.numel() >= 1
+    assert new_ids.dtype == num_used.dtype == torch.int32
     _check(lib().cs_kv_pages_compact(ctypes.byref(space.c), layer_begin, layer_end, ctypes.byref(tables.c), ctypes.byref(new_tables.c),
                                      _ptr(new_ids), _ptr(num_used), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                      _stream(stream)), "cs_kv_pages_compact")

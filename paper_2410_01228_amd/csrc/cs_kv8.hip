@@ -8,6 +8,7 @@
 // the attention kernels is exact, and the range of e4m3 (2^-9 to 448) leaves so much room below that a finer scale would
 // gain nothing: its steps are relative.
 #include <algorithm>
+#include <new>
 #include "cs_common.h"
 #include "cs_elem.h"
 #include "cs_plan.h"
@@ -374,6 +375,11 @@ static int append8(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch
     return check_launch("8-bit append kernel");
 }
 
+// The plan of an attention call, null where the host has no memory for one (no exception leaves a C entry).
+static const Plans* plans8(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D) {
+    try { return &plans_for(b, Hq, Hkv, D, 1, 1); } catch (const std::bad_alloc&) { return nullptr; }
+}
+
 static int attention_kv8(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch, const void* q, void* out, int32_t Hq, float softmax_scale,
                          void* workspace, size_t workspace_bytes, void* stream, bool f16) {
     int rc = validate_kv8(pool);
@@ -388,7 +394,9 @@ static int attention_kv8(const cs_kv8_pool* pool, int32_t layer, const cs_batch*
     if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return CS_ERR_INVALID_ARG;   // positive, finite
 
     const cs_kv_pool view = kv8_view(*pool);
-    const Plans& plans = plans_for(batch, Hq, pool->num_kv_heads, pool->head_dim, 1, 1);
+    const Plans* planned = plans8(batch, Hq, pool->num_kv_heads, pool->head_dim);
+    if (!planned) return hip_failed(hipErrorOutOfMemory, "launch plan");
+    const Plans& plans = *planned;
     const DecodePlan& d = plans.d;
     const PrefillPlan& p = plans.p;
     if (plans.need > 0 && (!workspace || ((uintptr_t)workspace & 15))) return CS_ERR_INVALID_ARG;
@@ -433,7 +441,8 @@ int cs_kv8_append_f16(const cs_kv8_pool* pool, int32_t layer, const cs_batch* ba
 size_t cs_paged_attention_kv8_workspace_bytes(const cs_batch* batch, int32_t Hq, int32_t Hkv, int32_t D) {
     if (attention_shape_ok(Hq, Hkv, D) != CS_OK) return 0;
     if (validate_batch(nullptr, batch) != CS_OK || batch->num_seqs == 0) return 0;
-    return plans_for(batch, Hq, Hkv, D, 1, 1).need;
+    const Plans* plans = plans8(batch, Hq, Hkv, D);
+    return plans ? plans->need : 0;
 }
 
 int cs_paged_attention_mixed_kv8(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch, const void* q, void* out, int32_t Hq,

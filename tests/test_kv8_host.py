@@ -206,3 +206,24 @@ def test_attention_plans_of_drawn_batches():
         assert cs.cs_paged_attention_kv8_workspace_bytes(b, hq, hkv, d) == x < 1 << 31
         cs.cs_paged_attention_workspace_bytes(b, hq, hkv, d)                        # (the 16-bit plan of the same lengths is another)
         assert cs.cs_paged_attention_kv8_workspace_bytes(b, hq, hkv, d) == x
+
+
+def test_the_binding_refuses_lists_that_are_too_short_or_of_another_type():
+    staging = cs.PageSpace.staging(torch.zeros((2, 4, 64), dtype=torch.uint8))
+    ids = torch.zeros(3, dtype=torch.int32)
+    for src, dst, n in ((ids, ids[:2], None), (ids[:1], None, 2), (ids.long(), ids, None), (None, ids.long(), None)):
+        with pytest.raises(AssertionError):
+            cs.cs_kv_pages_copy(staging, 0, src, staging, 0, dst, 2, n, stream=0)
+    tables = cs.PageTables(torch.zeros((2, 3), dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(4, dtype=torch.int32))
+    with pytest.raises(AssertionError):
+        cs.cs_kv_pages_fork(staging, 0, 2, tables, ids, ids, ids[:2], stream=0)
+    with pytest.raises(AssertionError):
+        cs.cs_kv_pages_fork(staging, 0, 2, tables, ids, ids.long(), ids, stream=0)
+    with pytest.raises(AssertionError):
+        cs.cs_kv_pages_free(tables, ids, ids, ids, stream=0)
+    with pytest.raises(AssertionError):
+        cs.cs_kv_pages_free(tables, ids, torch.zeros(4, dtype=torch.int32), ids[:0], stream=0)
+    with pytest.raises(AssertionError):
+        cs.cs_kv_pages_compact(staging, 0, 2, tables, tables, ids, ids, torch.zeros(256, dtype=torch.uint8), stream=0)
+    with pytest.raises(AssertionError):
+        cs.Pool8(torch.zeros(cs.cs_kv8_page_bytes(2, 64) * 3 - 1, dtype=torch.uint8), 1, 3, 2, 64)
