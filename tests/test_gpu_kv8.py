@@ -1,4 +1,6 @@
 """The 8-bit KV cache on the GPU: the append bit for bit, attention against fp64 over the values the codes stand for."""
+import types
+
 import numpy as np
 import pytest
 import torch
@@ -433,6 +435,45 @@ def test_chunks_over_many_windows_of_pages(ctx, new, D, dtype):
     w = filled(ctx, new, 1, D, 33, dtype)
     q = queries(w, 4)
     check_attention(w, 4, attend(w, 4, q), q)
+
+
+def drawn_pool(ctx, new, Hkv, D, seed, dtype):
+    """A world whose codes are drawn, not appended: for batches too large for the oracle's append."""
+    w = World([], [], Hkv, D, seed, dtype)
+    need = [-(-(c + n) // 16) for c, n in zip(ctx, new)]
+    w.ctx, w.new, w.P = list(ctx), list(new), sum(need)
+    w.cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    w.tables, perm, o = np.full((len(ctx), max(need)), -1, np.int32), w.rng.permutation(w.P).astype(np.int32), 0
+    for s, n in enumerate(need):
+        w.tables[s, :n] = perm[o:o + n]
+        o += n
+    w.pool = w.rng.integers(0, 256, (1, w.P, w.stride), np.uint8)
+    w.pool[(w.pool & 127) == 127] = 0
+    codes = 2 * Hkv * 16 * D
+    scales = np.exp2(w.rng.integers(-9, -6, (w.P, 2 * Hkv))).astype(np.float32)      # (values up to 3.5)
+    w.pool[0, :, codes:codes + 8 * Hkv] = scales.view(np.uint8)
+    return w
+
+
+@pytest.mark.parametrize("Hq,Hkv,decodes,chunks,dtype", [
+    (28, 4, (64, 1024, 8192), [(3276, 512), (9712, 512), (10901, 512), (6220, 512)], torch.bfloat16),    # tiles whole, decode work behind them
+    (40, 8, (10, 239, 956), [(6461, 576), (768, 861), (232, 761), (3545, 984)], torch.float16),          # two kernels
+    (40, 8, (10, 239, 956), [(6461, 576), (768, 861), (232, 761), (3545, 984)], torch.bfloat16),
+    (64, 8, (60, 500, 2000), [(3000, 300)], torch.float16)])
+def test_mixes_in_the_arrangement_that_the_host_takes(Hq, Hkv, decodes, chunks, dtype):
+    """Some decodes and the last rows of every chunk against the oracle; the other rows are numbers."""
+    r = np.random.default_rng(40)
+    n, lo, hi = decodes
+    w = drawn_pool([int(x) for x in r.integers(lo, hi, n)] + [c for c, _ in chunks], [1] * n + [q for _, q in chunks], Hkv, 128, 41, dtype)
+    q = queries(w, Hq // Hkv)
+    out = attend(w, Hq // Hkv, q)
+    assert torch.isfinite(out.float()).all()
+    check_attention(w, Hq // Hkv, out, q, seqs=[0, n // 2, n - 1])
+    for s in range(n, n + len(chunks)):                                  # a chunk's last rows: a shorter chunk on more context
+        t = w.new[s] - 6
+        tail = types.SimpleNamespace(Hkv=Hkv, D=128, dtype=dtype, pool=w.pool, layer=0, tables=w.tables[s:s + 1], ctx=[w.ctx[s] + t], new=[6], cu=np.array([0, 6]))
+        rows = slice(int(w.cu[s]) + t, int(w.cu[s + 1]))
+        check_attention(tail, Hq // Hkv, out[rows], q[rows])
 
 
 def test_two_graphs_share_a_workspace():
