@@ -533,3 +533,48 @@ def test_two_threads_on_streams_of_their_own():
     assert not failed, failed
     for x, outs in zip(want, got):
         assert all(torch.equal(out, x) for out in outs)
+
+
+def nans_of_v_in_every_step(w, G):
+    """A V that is not a number in every 32 keys of every sequence, each in a feature of its own (a step's kv head and feature are not
+    used again); which outputs see one.  Rows before the first token of a step keep its feature."""
+    want = np.zeros((w.T, w.Hkv * G, w.D), bool)
+    for s, (c, n) in enumerate(zip(w.ctx, w.new)):
+        for step in range(-(-(c + n) // 32)):
+            assert step < w.Hkv * w.D
+            token, g, d = min(32 * step + int(w.rng.integers(32)), c + n - 1), step % w.Hkv, step // w.Hkv
+            codes, _ = kv8.block(w.pool, 0, int(w.tables[s, token // 16]), 1, g, w.Hkv, w.D)
+            codes[kv8.v_index(token % 16, np.arange(d, d + 1))] = NAN_CODE | (128 if step & 1 else 0)
+            t0 = int(w.cu[s])
+            want[t0 + max(token - c, 0):t0 + n, g * G:(g + 1) * G, d] = True
+    return want
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cus", [2, 256])
+@pytest.mark.parametrize("ctx,new", [(64, 40), (100, 40), (0, 40), (500, 40), (1700, 40), (1733, 40), (991, 300), (3000, 33), (3021, 17)])
+def test_a_v_that_is_no_number_at_every_place_of_a_tile(ctx, new, cus, D, dtype):
+    """Tiles whole (2 CUs need no cuts) and cut into ranges (256): edges at odd and even steps, ranges of odd and even length."""
+    w = filled([ctx], [new], 2, D, 50, dtype)
+    want, q = nans_of_v_in_every_step(w, 3), queries(w, 3)
+    try:
+        cs.cs_debug_set_cu_count(cus)
+        out = attend(w, 3, q)
+    finally:
+        cs.cs_debug_set_cu_count(0)
+    assert np.array_equal(torch.isnan(out).cpu().numpy(), want) and not torch.isinf(out).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("mode", [0, 2, 3])
+def test_a_v_that_is_no_number_in_every_step_of_a_mix(mode, D, dtype):
+    w = filled([40, 500, 1700, 2100, 65, 960, 300], [1, 1, 40, 1, 70, 33, 1], 2, D, 51, dtype)
+    want, q = nans_of_v_in_every_step(w, 4), queries(w, 4)
+    try:
+        cs.cs_set_mixed_fusion(mode)
+        out = attend(w, 4, q)
+    finally:
+        cs.cs_set_mixed_fusion(1)
+    assert np.array_equal(torch.isnan(out).cpu().numpy(), want) and not torch.isinf(out).any()
