@@ -766,9 +766,10 @@ __device__ __forceinline__ void prefill_tile(
     };
     // 8-bit pools, where a masked step held a V that is not a number: the outputs that see it become NaN, feature by feature, by a
     // product of ones -- where the V is none, by where the mask lets a row look.  The codes are read again from the pool, from
-    // the first masked step on: the steady state ends a step or two before the edge, or before the end of a range.
-    auto spread_nans = [&](int32_t first_masked) {
-        for (int32_t step = first_masked; step < step_end; ++step) {
+    // two steps before the edge, or before the end of a range, on: the steady state below leaves one or two to masked ones.  (All
+    // rows see those; a variable of the loop, kept alive to here, has the fused kernels spill 60 registers.)
+    auto spread_nans = [&]() {
+        for (int32_t step = max(step_begin, min(first_edge, step_end) - 2); step < step_end; ++step) {
             const int32_t entry = kStepPages * step + (lane >> 5), key0 = step * kKeysPerStep + (lane >> 5) * 16 + ((lane >> 4) & 1) * 8;
             const int32_t id = entry < n_pages ? table[entry] : 0;
             const char* v = (const char*)layer_base + (int64_t)((id < 0 || id >= num_pages) ? 0 : id) * page_stride * 2
@@ -809,7 +810,6 @@ __device__ __forceinline__ void prefill_tile(
         iteration(std::false_type{}, std::false_type{}, i, x, xb);
         iteration(std::false_type{}, std::false_type{}, i + 1, xb, x);
     }
-    const int32_t first_masked = i;
     for (; i + 1 < step_end; ++i) {
         iteration(std::true_type{}, std::false_type{}, i, x, xb);
 #pragma unroll
@@ -821,7 +821,7 @@ __device__ __forceinline__ void prefill_tile(
     if (kPriority) __builtin_amdgcn_s_setprio(0);
     wait_vmcnt<0>();                                   // no copy may outlive the workgroup's LDS
     if constexpr (kEight) {
-        if (saw_nan) spread_nans(first_masked);
+        if (saw_nan) spread_nans();
     }
 
     // ---- a cut tile leaves the partial of its range: unnormalised output, running max and sum per
