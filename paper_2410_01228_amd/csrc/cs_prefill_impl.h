@@ -113,21 +113,12 @@ __device__ __forceinline__ void lds_dma4_lane_addr(uint64_t addr, void* dst_wave
                  :: "s"(lds_addr), "v"(addr) : "memory", "m0");
 }
 
-// max(a, b, c) in one instruction.  fmaxf() makes the compiler canonicalise every operand
-// first (one extra v_max per value, to quiet signalling NaNs); the scores need no such care.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
+// The largest of eight scores (NaN if one of them is), made of instructions that the compiler knows (v_maximum3_f32, three values
+// each, with none of the canonicalising v_max that fmaxf() needs per value): no hardware waits for a matrix instruction whose
+// results a vector instruction reads, so the compiler has to keep the distance, and inside inline assembly it does not see the reads.
+// (As asm v_max3_f32 these were one instruction behind the 8-bit product of 128 values: at head dim 64 single rows
+// read a maximum from before it.)
 __device__ __forceinline__ float max8(const float (&x)[8]) {
-    return max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
-}
-// The same as instructions that the compiler knows (v_maximum3_f32; NaN if one of them is), so that it keeps them as far behind
-// the matrix instruction whose results they read as they have to be: no hardware waits for that.  An 8-bit product of
-// 128 values takes twice the passes of a 16-bit one of 32, and the asm above was put one instruction behind it: at head
-// dim 64 single rows read a maximum from before the product.
-__device__ __forceinline__ float maximum8(const float (&x)[8]) {
     auto three = [](float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); };
     return three(three(x[0], x[1], x[2]), three(x[3], x[4], x[5]), three(x[6], x[7], x[7]));
 }
@@ -552,12 +543,12 @@ __device__ __forceinline__ void prefill_tile(
         bool need = false;
 #pragma unroll
         for (int c = 0; c < kNCT; ++c) {
-            need |= (kEight ? maximum8(xs[c]) : max8(xs[c])) > thr[c];
+            need |= max8(xs[c]) > thr[c];
         }
         if (__any(need)) {
 #pragma unroll
             for (int c = 0; c < kNCT; ++c) {
-                float m = kEight ? maximum8(xs[c]) : max8(xs[c]);
+                float m = max8(xs[c]);
                 m = fmaxf(m, __shfl_xor(m, 16, 64));
                 m = fmaxf(m, __shfl_xor(m, 32, 64));
                 if constexpr (kFold) {

@@ -123,3 +123,76 @@ def test_a_lone_workgroup_loads_no_page_behind_its_last(tmp_path, D, page):
     # loads: the first page's in front of the loop, the next one's in it; products: a page's in the loop, the last one's behind it
     assert len(re.findall(r"global_load_dwordx[24] .*\bnt\b", text)) == 2 * (D // 32 + D // 16)
     assert len(re.findall(r"v_mfma_f32_16x16x32", text)) == 2 * (D // 32)
+
+
+MATRIX_RESULT_WAITS = 20        # wait states that cover every product used here (16 passes; those of 4 passes need 8)
+
+
+def registers(operand):
+    m = re.match(r"[-|]*([va])\[(\d+):(\d+)\]", operand)
+    if m:
+        return {m.group(1) + str(r) for r in range(int(m.group(2)), int(m.group(3)) + 1)}
+    m = re.match(r"[-|]*([va])(\d+)\b", operand)
+    return {m.group(1) + m.group(2)} if m else set()
+
+
+def matrix_results_read_in_asm(asm_text):
+    """(line number, instruction, wait states) of every instruction inside an inline-asm block that reads a register fewer than
+    MATRIX_RESULT_WAITS behind the matrix instruction that wrote it: nothing waits there, the hardware does not and the
+    compiler does not look into the block.  (Instructions are counted in the order of the text.)"""
+    found, written, states, inside = [], {}, 0, False
+    for number, line in enumerate(asm_text.split("\n"), 1):
+        t = line.strip()
+        if "ASMSTART" in t or "ASMEND" in t:
+            inside = "ASMSTART" in t
+            continue
+        if not t or t[0] in ";.#" or t.split(";")[0].strip().endswith(":"):
+            if t.startswith(".Lfunc_end"):
+                written = {}
+            continue
+        t = t.split(";")[0].strip()
+        op = t.split()[0]
+        states += int(t.split()[1], 0) + 1 if op == "s_nop" else 1
+        operands = [a.strip() for a in t[len(op):].split(",")]
+        if op.startswith(("v_mfma", "v_smfmac")):
+            written.update({r: states for r in registers(operands[0])})
+            continue
+        stores = op.startswith(("global_store", "global_atomic", "buffer_store", "ds_write", "global_load_lds"))
+        for a in operands if stores else operands[1:]:
+            for r in registers(a):
+                if inside and states - written.get(r, -MATRIX_RESULT_WAITS) < MATRIX_RESULT_WAITS:
+                    found.append((number, t, states - written[r]))
+        if not stores and op[0] != "s":
+            for r in registers(operands[0]):
+                written.pop(r, None)
+    return found
+
+
+def test_scanner_sees_a_planted_read_of_a_matrix_result():
+    bad = """
+	v_mfma_f32_16x16x32_bf16 v[4:7], v[0:3], v[8:11], 0
+	s_nop 3
+	v_add_u32_e32 v20, v21, v22
+	;;#ASMSTART
+	v_max3_f32 v30, v4, v5, v6
+	;;#ASMEND
+"""
+    assert [f[1:] for f in matrix_results_read_in_asm(bad)] == [("v_max3_f32 v30, v4, v5, v6", 6)] * 3
+    assert matrix_results_read_in_asm(bad.replace("s_nop 3", "s_nop 15\n\ts_nop 4")) == []
+    assert matrix_results_read_in_asm(bad.replace("v_add_u32_e32 v20, v21, v22", "v_mov_b32_e32 v4, 0\n\tv_mov_b32_e32 v5, 0\n\tv_mov_b32_e32 v6, 0")) == []
+    assert matrix_results_read_in_asm(bad.replace(";;#ASM", ";;#")) == []
+
+
+@pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"), reason="no hipcc")
+@pytest.mark.parametrize("src", USERS + ["cs_decode.hip"])
+def test_no_asm_reads_a_matrix_result_that_may_not_be_there(tmp_path, src):
+    hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+    out = tmp_path / (src + ".s")
+    cmd = [hipcc, "--offload-arch=gfx950", "-O3", "-std=c++17", "-I" + os.path.join(ROOT, "include"),
+           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-S", "--cuda-device-only", "-o", str(out),
+           os.path.join(CSRC, src)]
+    subprocess.run(cmd, check=True, stdout=subprocess.DEVNULL, stderr=subprocess.DEVNULL)
+    text = out.read_text()
+    assert text.count("v_mfma_f32") > 100
+    hazards = matrix_results_read_in_asm(text)
+    assert hazards == [], "%d reads, the closest %r" % (len(hazards), min(hazards, key=lambda f: f[2]))
