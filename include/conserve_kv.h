@@ -448,7 +448,8 @@ typedef struct {
  * second one for more layers would count the pages again (cs_kv_pages_copy takes a page's other layers along).
  * parents, children, fresh_pages: device [n].  A parent may be named more often; children must be distinct and no
  * parents, fresh pages distinct and free.  A fork with a row outside the tables is skipped; one that needs a fresh
- * page and has none inside the pool makes a child of the full pages alone. */
+ * page and has none inside the pool, or whose parent's unfinished page lies outside it, makes a child of the full pages
+ * alone (the fresh page is not touched then). */
 int cs_kv_pages_fork(const cs_page_space* space, int32_t layer_begin, int32_t layer_end,
                      const cs_page_tables* tables, const int32_t* parents, const int32_t* children,
                      const int32_t* fresh_pages, int32_t n, void* stream);

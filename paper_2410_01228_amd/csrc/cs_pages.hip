@@ -104,14 +104,13 @@ __global__ __launch_bounds__(kLanes) void pages_fork_kernel(const Pages pool, in
     const int32_t full = n / t.page_size;
     const bool tail = n > full * t.page_size;
     const int32_t* from = t.entries + (int64_t)parent * t.max_blocks;
-    const bool copied = tail && pool.has(fresh);
+    const int32_t last = tail ? from[full] : -1;
+    const bool copied = pool.has(last) && pool.has(fresh);
     if ((int32_t)blockIdx.y < layers) {
-        if (!copied) return;
-        const int32_t last = from[full];
-        if (pool.has(last)) copy_chunk<kLanes, kForkRuns, true>(pool.at(blockIdx.y, fresh), pool.at(blockIdx.y, last), c, chunks_per_page, page_bytes);
+        if (copied) copy_chunk<kLanes, kForkRuns, true>(pool.at(blockIdx.y, fresh), pool.at(blockIdx.y, last), c, chunks_per_page, page_bytes);
         return;
     }
-    if (tail && !copied) n = full * t.page_size;                  // no page for the rest: the child ends at its last full one
+    if (!copied) n = full * t.page_size;                          // no page for the rest, or no rest: the child ends at its last full one
     int32_t* to = t.entries + (int64_t)child * t.max_blocks;
     for (int32_t e = c * kLanes + threadIdx.x; e < t.max_blocks; e += chunks_per_page * kLanes) {
         int32_t id = -1;

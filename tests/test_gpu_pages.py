@@ -351,3 +351,24 @@ def test_a_serving_loop(D):
     step({1: 3, 2: 1, 3: 17})
     release([1, 2, 3])
     assert int(tables.ref_counts.abs().max()) == 0 and sorted(free) == list(range(P))
+
+
+@pytest.mark.parametrize("bad", [-1, 40, 2 ** 31 - 1])
+def test_a_fork_of_an_unfinished_page_that_is_not_there(bad):
+    """The child ends at the parent's last full page: the fresh page holds nothing of the parent's, and stays free."""
+    r = np.random.default_rng(6)
+    tables, lens, counts, spare = world(r, [50, 9, 33, 0, 0, 0], 40, 8)
+    a = noise(r, 2, 40, 256)
+    tables[0, 3], tables[1, 0] = bad, bad                                # both unfinished
+    counts[:] = 0
+    np.add.at(counts, tables[(tables >= 0) & (tables < 40)], 1)
+    s, t = space_of(a, 256)
+    d = cs.PageTables(dev(tables), dev(lens), dev(counts))
+    cs.cs_kv_pages_fork(s, 0, 2, d, dev([0, 1, 2]), dev([3, 4, 5]), dev(spare[:3]))
+    kv8.ref_fork(a, 0, 2, tables, lens, counts, [2], [5], spare[2:3])    # the third is an ordinary one
+    counts[tables[0, :3]] += 1
+    tables[3, :3] = tables[0, :3]
+    lens[3], lens[4] = 48, 0
+    assert np.array_equal(t.cpu().numpy(), a)
+    for got, want in ((d.block_tables, tables), (d.lens, lens), (d.ref_counts, counts)):
+        assert np.array_equal(got.cpu().numpy(), want)
