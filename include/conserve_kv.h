@@ -381,8 +381,9 @@ size_t cs_kv8_page_bytes(int32_t num_kv_heads, int32_t head_dim);
  * and where e rises, the codes of the earlier tokens are divided by the rise and rounded again (exact
  * unless they fall below 2^-6 of the new scale).  Pages that are full never change, slots behind the last
  * token are left as they are, and a token's code depends only on its own value and its block's scale.
- * Infinities do not count for e and end as the largest code; a NaN stays one.  fp16: values beyond 61440, the
- * largest multiple of an e4m3 value that half precision holds, are rounded to it.  A page must not be appended to by two
+ * Values beyond the largest multiple of an e4m3 value that the type holds
+ * (bf16 240 * 2^120, fp16 61440) are rounded to it, so that no finite value comes back as an infinity.  Infinities of
+ * bf16 do not count for e and end at the largest value in reach (448 * 2^e, or that limit); a NaN stays one.  A page must not be appended to by two
  * calls at once, nor by two sequences of one (cs_kv_pages_fork gives each its own).  T == 0 is a no-op. */
 int cs_kv8_append(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch,
                   const void* k_new, const void* v_new, void* stream);
@@ -392,6 +393,8 @@ int cs_kv8_append_f16(const cs_kv8_pool* pool, int32_t layer, const cs_batch* ba
 /* cs_paged_attention_mixed over an 8-bit pool: K_s and V_s are code * scale, read through block_tables[s] and
  * widened to the type of q and out (bf16; fp16 in the _f16 call) without rounding.  (Half precision: a value under 2^-14
  * keeps what half precision has for it, and a scale whose codes pass 61440 is not one that cs_kv8_append_f16 makes.)
+ * (The sums of weights times V are fp32 and normalised at the end, a chunk's weights up to 2^6: they overflow for a V
+ * around 2^121 and more, in either cache.)
  * A row that sees a K or V, or has a Q, that is no number is none; other rows are not touched by it.  Everything else is as there
  * (cs_set_decode_pages_ahead has no say: 8-bit decode has one depth).  workspace: at least cs_paged_attention_kv8_workspace_bytes(). */
 size_t cs_paged_attention_kv8_workspace_bytes(const cs_batch* batch, int32_t num_q_heads,

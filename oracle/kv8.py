@@ -15,6 +15,7 @@ PAGE = 16
 LEAST = -100              # exponent of the smallest scale
 MOST_CODE = 448.0
 MOST_HALF = 61440.0       # largest multiple of an e4m3 value that half precision holds
+MOST_BF16 = 240 * 2.0 ** 120      # and bf16
 
 
 def _table():
@@ -91,6 +92,8 @@ def ref_append(pool, layer, tables, ctx_lens, cu_q_lens, k_new, v_new, Hkv, D, h
                     x = np.asarray(rows[t0 + lo - c:t0 + hi - c, h], np.float64)
                     if half:
                         x = np.clip(x, -MOST_HALF, MOST_HALF)
+                    else:                                             # (infinities do not count, and end at the largest value in reach)
+                        x = np.where(np.isinf(x), x, np.clip(x, -MOST_BF16, MOST_BF16))
                     size = np.abs(x[np.isfinite(x)])
                     e = exponent_for(size.max() if size.size else 0.0)
                     if held:
@@ -99,6 +102,8 @@ def ref_append(pool, layer, tables, ctx_lens, cu_q_lens, k_new, v_new, Hkv, D, h
                             at = index(np.arange(held)[:, None], d)
                             codes[at] = encode(VALUES[codes[at]] * 2.0 ** (before - e))
                         e = max(e, before)
+                    if not half:
+                        x = np.clip(x, -MOST_BF16, MOST_BF16)
                     codes[index(np.arange(lo, hi)[:, None] - j * PAGE, d)] = encode(x * 2.0 ** -e)
                     scale[0] = 2.0 ** e
     return pool

@@ -20,22 +20,24 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int32_t kLeastExponent = -100, kMostExponent = 120;
 constexpr float kMostCode = 448.f;
 constexpr float kMostHalf = 61440.f;         // the largest value of 4 significant bits that half precision holds
+constexpr float kMostBf16 = 0x1.ep127f;      // and bf16: 240 * 2^120 (above 248 * 2^120 the nearest code stands for 2^128)
 
 // Where the blocks' scales begin in a page, in bytes.
 __host__ __device__ inline int32_t scales_offset(int32_t Hkv, int32_t D) { return 2 * Hkv * (kPage * D); }
 
-// The new rows' element type.  kMost: a block whose largest value is beyond it is a rare one (rare_size, rare_limit): bf16
-// infinities, which end at the largest code and say nothing about the scale; fp16 values beyond kMostHalf, which end there.
+// The new rows' element type.  kMost: a block whose largest value is beyond it is a rare one (rare_size, rare_limit): values beyond the
+// largest one of 4 significant bits, which end there, and infinities (bf16: they say nothing about the scale, and end at the
+// block's largest code; fp16: values beyond kMostHalf like others).
 struct RowBf16 {
-    static constexpr float kMost = 3.4e38f;
-    static constexpr uint32_t kMostBits = 0x7f7f;
+    static constexpr float kMost = kMostBf16;
+    static constexpr uint32_t kMostBits = 0x7f70;
     static __device__ __forceinline__ float value(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
     static __device__ __forceinline__ void widen(uint32_t w, float& a, float& b) {
         a = __builtin_bit_cast(float, w << 16);
         b = __builtin_bit_cast(float, w & 0xffff0000u);
     }
-    static __device__ __forceinline__ float rare_size(float x) { return fabsf(x) <= kMost ? fabsf(x) : 0.f; }
-    static __device__ __forceinline__ float rare_limit(float) { return kMostCode; }
+    static __device__ __forceinline__ float rare_size(float x) { return fabsf(x) < INFINITY ? fminf(fabsf(x), kMost) : 0.f; }
+    static __device__ __forceinline__ float rare_limit(float inv) { return fminf(kMostCode, kMost * inv); }
 };
 struct RowF16 {
     typedef _Float16 x2 __attribute__((ext_vector_type(2)));

@@ -578,3 +578,36 @@ def test_a_v_that_is_no_number_in_every_step_of_a_mix(mode, D, dtype):
     finally:
         cs.cs_set_mixed_fusion(1)
     assert np.array_equal(torch.isnan(out).cpu().numpy(), want) and not torch.isinf(out).any()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("ctx,new", [([6, 0, 16], [1, 1, 1]), ([0, 6, 33], [24, 9, 2])])
+def test_append_of_the_largest_values_of_bf16(ctx, new, D):
+    """From 248 * 2^120 on the nearest code at the block's scale, 256, would stand for 2^128, an infinity: 240 it is.  The rows
+    that do not see such a V stay what they are (0 * infinity would be no number)."""
+    w = World(ctx, new, 2, D, 52)
+    k, v = w.rows(w.T), w.rows(w.T)
+    most = float(torch.finfo(torch.bfloat16).max)
+    for s in range(3):
+        row = int(w.cu[s + 1]) - 1                                       # a sequence's last token
+        v[row, 0, 0], v[row, 0, 3], v[row, 0, 5], v[row, 0, 6] = most, -most, 248 * 2.0 ** 120, 240 * 2.0 ** 120
+        v[row, 0, 7] = np.inf
+    w.pool[0] = np.where((w.pool[0] & 127) == 127, 0, w.pool[0])
+    got, want = w.append(k, v)
+    assert same_codes(got, want, 2, D)
+    w.pool = got
+    for s in range(3):
+        _, V = kv8.read_logical(got, 0, w.tables[s], ctx[s] + new[s], 2, D)
+        assert list(V[-1, 0, [0, 3, 5, 6, 7]]) == [240 * 2.0 ** 120 * sign for sign in (1, -1, 1, 1, 1)]
+    q = queries(w, 2)
+    out = attend(w, 2, q)
+    for s in range(3):
+        # A chunk's weights are relative to a maximum that may lie 2^6 below the scores', and its sums are normalised at the end: 2^6 * 240 *
+        # 2^120 is beyond fp32, so the one row that sees these values may say so, in their features.  All others, and
+        # decodes (whose weights are at most 1, with one such value a feature), are within the roundings.
+        rows = slice(int(w.cu[s]), int(w.cu[s + 1]) - (new[s] > 1))
+        few = types.SimpleNamespace(Hkv=2, D=D, dtype=w.dtype, pool=w.pool, layer=0, tables=w.tables[s:s + 1], ctx=[ctx[s]], new=[rows.stop - rows.start], cu=np.array([0]))
+        check_attention(few, 2, out[rows], q[rows])
+        large = out[int(w.cu[s + 1]) - 1].clone()
+        large[:2, [0, 3, 5, 6, 7]] = 0
+        assert torch.isfinite(large).all()
