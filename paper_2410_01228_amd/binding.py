@@ -256,7 +256,7 @@ class Pool8:
         self.page_bytes = cs_kv8_page_bytes(Hkv, D)
         self.page_stride = self.page_bytes if page_stride is None else page_stride
         self.layer_stride = P * self.page_stride if layer_stride is None else layer_stride
-        assert tensor.numel() * tensor.element_size() >= (L - 1) * self.layer_stride + P * self.page_stride
+        assert tensor.is_contiguous() and tensor.numel() * tensor.element_size() >= (L - 1) * self.layer_stride + P * self.page_stride
         self.c = cs_kv8_pool(_ptr(tensor), L, P, Hkv, D, self.layer_stride, self.page_stride)
         self.L, self.P, self.Hkv, self.D = L, P, Hkv, D
 
@@ -293,7 +293,7 @@ class PageTables:
 
     def __init__(self, block_tables: torch.Tensor, lens: torch.Tensor, ref_counts: torch.Tensor, page_size: int = PAGE):
         assert block_tables.dim() == 2 and lens.shape == block_tables.shape[:1] and ref_counts.dim() == 1
-        assert all(t.dtype == torch.int32 and t.is_contiguous() for t in (block_tables, lens, ref_counts))
+        assert all(t.dtype == torch.int32 and t.is_contiguous() and t.device == lens.device for t in (block_tables, lens, ref_counts))
         self.block_tables, self.lens, self.ref_counts = block_tables, lens, ref_counts
         self.c = cs_page_tables(_ptr(block_tables), _ptr(lens), _ptr(ref_counts), int(block_tables.shape[0]), int(block_tables.shape[1]),
                                 int(ref_counts.numel()), page_size)
@@ -549,17 +549,31 @@ def run_layers_workspace_for(batch: Batch, num_online_seqs: int, Hq: int, Hkv: i
     return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
 
 
+# What the calls below take as bare addresses: contiguous, and as long as the kernels read or write.  (Each question to a
+# tensor costs the host 0.1 us of a call's nine, so no more are asked than a mistake could answer wrongly in silence.)
+def _rows(t: torch.Tensor, n: int) -> int:
+    assert t.is_contiguous() and t.numel() >= n
+    return t.data_ptr()
+
+
+def _list(t: torch.Tensor, n: int) -> int:
+    assert t.dtype is torch.int32 and t.is_contiguous() and t.numel() >= n
+    return t.data_ptr()
+
+
 def cs_kv8_page_bytes(Hkv: int, D: int) -> int:
     return int(lib().cs_kv8_page_bytes(Hkv, D))
 
 
 def cs_kv8_append(pool: Pool8, layer: int, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor, stream=None):
-    _check(lib().cs_kv8_append(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _ptr(k_new), _ptr(v_new),
+    n = batch.c.num_tokens * pool.Hkv * pool.D
+    _check(lib().cs_kv8_append(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _rows(k_new, n), _rows(v_new, n),
                                _stream(stream)), "cs_kv8_append")
 
 
 def cs_kv8_append_f16(pool: Pool8, layer: int, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor, stream=None):
-    _check(lib().cs_kv8_append_f16(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _ptr(k_new), _ptr(v_new),
+    n = batch.c.num_tokens * pool.Hkv * pool.D
+    _check(lib().cs_kv8_append_f16(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _rows(k_new, n), _rows(v_new, n),
                                    _stream(stream)), "cs_kv8_append_f16")
 
 
@@ -575,7 +589,8 @@ def workspace_for_kv8(batch: Batch, Hq: int, Hkv: int, D: int, device="cuda") ->
 def cs_paged_attention_mixed_kv8(pool: Pool8, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor,
                                  Hq: int, softmax_scale: float, workspace: Optional[torch.Tensor], stream=None):
     wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().cs_paged_attention_mixed_kv8(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _ptr(q), _ptr(out),
+    n = batch.c.num_tokens * Hq * pool.D
+    _check(lib().cs_paged_attention_mixed_kv8(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _rows(q, n), _rows(out, n),
                                               Hq, softmax_scale, _ptr(workspace), wb, _stream(stream)),
            "cs_paged_attention_mixed_kv8")
 
@@ -583,7 +598,8 @@ def cs_paged_attention_mixed_kv8(pool: Pool8, layer: int, batch: Batch, q: torch
 def cs_paged_attention_mixed_kv8_f16(pool: Pool8, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor,
                                      Hq: int, softmax_scale: float, workspace: Optional[torch.Tensor], stream=None):
     wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().cs_paged_attention_mixed_kv8_f16(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _ptr(q), _ptr(out),
+    n = batch.c.num_tokens * Hq * pool.D
+    _check(lib().cs_paged_attention_mixed_kv8_f16(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _rows(q, n), _rows(out, n),
                                                   Hq, softmax_scale, _ptr(workspace), wb, _stream(stream)),
            "cs_paged_attention_mixed_kv8_f16")
 
@@ -593,33 +609,29 @@ def cs_kv_pages_copy(src: PageSpace, src_layer: int, src_ids: Optional[torch.Ten
     """n: by default the length of the id lists; needed where both are None."""
     if n is None:
         n = (src_ids if src_ids is not None else dst_ids).numel()
-    assert all(t is None or (t.dtype == torch.int32 and t.numel() >= n) for t in (src_ids, dst_ids))
-    _check(lib().cs_kv_pages_copy(ctypes.byref(src.c), src_layer, _ptr(src_ids), ctypes.byref(dst.c), dst_layer, _ptr(dst_ids),
-                                  num_layers, n, _stream(stream)), "cs_kv_pages_copy")
+    _check(lib().cs_kv_pages_copy(ctypes.byref(src.c), src_layer, None if src_ids is None else _list(src_ids, n), ctypes.byref(dst.c), dst_layer,
+                                  None if dst_ids is None else _list(dst_ids, n), num_layers, n, _stream(stream)), "cs_kv_pages_copy")
 
 
 def cs_kv_pages_fork(space: PageSpace, layer_begin: int, layer_end: int, tables: PageTables, parents: torch.Tensor,
                      children: torch.Tensor, fresh_pages: torch.Tensor, stream=None):
-    assert parents.numel() == children.numel() == fresh_pages.numel()
-    assert parents.dtype == children.dtype == fresh_pages.dtype == torch.int32
-    _check(lib().cs_kv_pages_fork(ctypes.byref(space.c), layer_begin, layer_end, ctypes.byref(tables.c), _ptr(parents), _ptr(children),
-                                  _ptr(fresh_pages), parents.numel(), _stream(stream)), "cs_kv_pages_fork")
+    n = parents.numel()
+    assert n == children.numel() == fresh_pages.numel()
+    _check(lib().cs_kv_pages_fork(ctypes.byref(space.c), layer_begin, layer_end, ctypes.byref(tables.c), _list(parents, n), _list(children, n),
+                                  _list(fresh_pages, n), n, _stream(stream)), "cs_kv_pages_fork")
 
 
 def cs_kv_pages_free(tables: PageTables, rows: torch.Tensor, freed: torch.Tensor, num_freed: torch.Tensor, stream=None):
-    assert freed.numel() >= tables.ref_counts.numel() and num_freed.numel() >= 1
-    assert rows.dtype == freed.dtype == num_freed.dtype == torch.int32
-    _check(lib().cs_kv_pages_free(ctypes.byref(tables.c), _ptr(rows), rows.numel(), _ptr(freed), _ptr(num_freed), _stream(stream)),
-           "cs_kv_pages_free")
+    n = rows.numel()
+    _check(lib().cs_kv_pages_free(ctypes.byref(tables.c), _list(rows, n), n, _list(freed, tables.c.num_pages), _list(num_freed, 1),
+                                  _stream(stream)), "cs_kv_pages_free")
 
 
 def cs_kv_pages_compact(space: PageSpace, layer_begin: int, layer_end: int, tables: PageTables, new_tables: PageTables,
                         new_ids: torch.Tensor, num_used: torch.Tensor, workspace: torch.Tensor, stream=None):
-    assert new_ids.numel() >= tables.ref_counts.numel() and num_used.numel() >= 1
-    assert new_ids.dtype == num_used.dtype == torch.int32
     _check(lib().cs_kv_pages_compact(ctypes.byref(space.c), layer_begin, layer_end, ctypes.byref(tables.c), ctypes.byref(new_tables.c),
-                                     _ptr(new_ids), _ptr(num_used), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                     _stream(stream)), "cs_kv_pages_compact")
+                                     _list(new_ids, tables.c.num_pages), _list(num_used, 1), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size(), _stream(stream)), "cs_kv_pages_compact")
 
 
 def compact_workspace_for(space: PageSpace, device="cuda") -> torch.Tensor:

@@ -227,3 +227,39 @@ def test_the_binding_refuses_lists_that_are_too_short_or_of_another_type():
         cs.cs_kv_pages_compact(staging, 0, 2, tables, tables, ids, ids, torch.zeros(256, dtype=torch.uint8), stream=0)
     with pytest.raises(AssertionError):
         cs.Pool8(torch.zeros(cs.cs_kv8_page_bytes(2, 64) * 3 - 1, dtype=torch.uint8), 1, 3, 2, 64)
+
+
+def test_the_binding_refuses_views_that_the_kernels_would_read_past():
+    """Every second entry of a list, heads out of wider rows, too few rows: the calls take bare addresses, and would read the neighbours."""
+    staging, ids = cs.PageSpace.staging(torch.zeros((2, 4, 64), dtype=torch.uint8)), torch.zeros(4, dtype=torch.int32)
+    bad = torch.zeros(8, dtype=torch.int32)[::2]
+    tables = cs.PageTables(torch.zeros((2, 3), dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(4, dtype=torch.int32))
+    scratch = torch.zeros(256, dtype=torch.uint8)
+    for call in (lambda: cs.cs_kv_pages_copy(staging, 0, bad, staging, 0, ids, 2, stream=0),
+                 lambda: cs.cs_kv_pages_copy(staging, 0, None, staging, 0, bad, 2, stream=0),
+                 lambda: cs.cs_kv_pages_fork(staging, 0, 2, tables, bad, ids, ids, stream=0),
+                 lambda: cs.cs_kv_pages_fork(staging, 0, 2, tables, ids, bad, ids, stream=0),
+                 lambda: cs.cs_kv_pages_fork(staging, 0, 2, tables, ids, ids, bad, stream=0),
+                 lambda: cs.cs_kv_pages_free(tables, bad, ids, ids, stream=0),
+                 lambda: cs.cs_kv_pages_free(tables, ids, bad, ids, stream=0),
+                 lambda: cs.cs_kv_pages_free(tables, ids, ids, bad, stream=0),
+                 lambda: cs.cs_kv_pages_compact(staging, 0, 2, tables, tables, bad, ids, scratch, stream=0),
+                 lambda: cs.cs_kv_pages_compact(staging, 0, 2, tables, tables, ids, bad, scratch, stream=0)):
+        with pytest.raises(AssertionError):
+            call()
+    with pytest.raises(AssertionError):
+        cs.PageTables(torch.zeros((2, 3), dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(4, dtype=torch.int32, device="meta"))
+    pool = cs.Pool8(torch.zeros(cs.cs_kv8_page_bytes(2, 64) * 3, dtype=torch.uint8), 1, 3, 2, 64)
+    b = host_batch([0], [5])
+    good = torch.zeros((5, 2, 64), dtype=torch.bfloat16)
+    wider = torch.zeros((5, 6, 64), dtype=torch.bfloat16)
+    for rows in (wider[:, :2], good[:4]):
+        for f16 in ("", "_f16"):
+            append, attend = getattr(cs, "cs_kv8_append" + f16), getattr(cs, "cs_paged_attention_mixed_kv8" + f16)
+            for k, v in ((rows, good), (good, rows)):
+                with pytest.raises(AssertionError):
+                    append(pool, 0, b, k, v, stream=0)
+                with pytest.raises(AssertionError):
+                    attend(pool, 0, b, k, v, 2, 0.125, None, stream=0)
+    with pytest.raises(AssertionError):
+        cs.Pool8(torch.zeros((3, 2 * cs.cs_kv8_page_bytes(2, 64)), dtype=torch.uint8)[:, ::2], 1, 3, 2, 64)
