@@ -383,7 +383,8 @@ size_t cs_kv8_page_bytes(int32_t num_kv_heads, int32_t head_dim);
  * token are left as they are, and a token's code depends only on its own value and its block's scale.
  * Values beyond the largest multiple of an e4m3 value that the type holds
  * (bf16 240 * 2^120, fp16 61440) are rounded to it, so that no finite value comes back as an infinity.  Infinities of
- * bf16 do not count for e and end at the largest value in reach (448 * 2^e, or that limit); a NaN stays one.  A page must not be appended to by two
+ * bf16 do not count for e and end at the largest value in reach (448 * 2^e, or that limit); one of fp16 is a value beyond
+ * 61440 like others, so it sets e to 8, and values of its block below 4 lose bits to it; a NaN stays one.  A page must not be appended to by two
  * calls at once, nor by two sequences of one (cs_kv_pages_fork gives each its own).  T == 0 is a no-op. */
 int cs_kv8_append(const cs_kv8_pool* pool, int32_t layer, const cs_batch* batch,
                   const void* k_new, const void* v_new, void* stream);

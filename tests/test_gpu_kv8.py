@@ -611,3 +611,19 @@ def test_append_of_the_largest_values_of_bf16(ctx, new, D):
         large = out[int(w.cu[s + 1]) - 1].clone()
         large[:2, [0, 3, 5, 6, 7]] = 0
         assert torch.isfinite(large).all()
+
+
+@pytest.mark.parametrize("new", [1, 5])
+def test_what_an_infinity_becomes(new):
+    """bf16: the largest code at the scale of the block's other values; fp16: 61440, whatever the others are."""
+    for dtype, exponent, value in ((torch.bfloat16, -8, 448 * 2.0 ** -8), (torch.float16, 8, 61440.0)):
+        w = World([0], [new], 1, 64, 53, dtype)
+        k = np.ones((new, 1, 64))
+        k[-1, 0, 9] = -np.inf
+        got, _ = w.append(k, np.ones((new, 1, 64)))
+        assert kv8.block(got, 0, int(w.tables[0, 0]), 0, 0, 1, 64)[1][0] == 2.0 ** exponent
+        K, V = kv8.read_logical(got, 0, w.tables[0], new, 1, 64)
+        want = np.ones((new, 1, 64))
+        assert np.array_equal(V, want)
+        want[-1, 0, 9] = -value
+        assert np.array_equal(K, want)
