@@ -394,6 +394,7 @@ int cs_kv8_append_f16(const cs_kv8_pool* pool, int32_t layer, const cs_batch* ba
 /* cs_paged_attention_mixed over an 8-bit pool: K_s and V_s are code * scale, read through block_tables[s] and
  * widened to the type of q and out (bf16; fp16 in the _f16 call) without rounding.  (Half precision: a value under 2^-14
  * keeps what half precision has for it, and a scale whose codes pass 61440 is not one that cs_kv8_append_f16 makes.)
+ * (Chunks, bf16: values of a row of q below 2^-13.8 of its largest are held to 2^-21.8 of that largest.)
  * (The sums of weights times V are fp32 and normalised at the end, a chunk's weights up to 2^6: they overflow for a V
  * around 2^121 and more, in either cache.)
  * A row that sees a K or V, or has a Q, that is no number is none; other rows are not touched by it.  Everything else is as there

@@ -109,8 +109,10 @@ template <class E> struct Kv8 : E {
 // Q as codes, for products with K's codes on the 8-bit matrix instruction (a tile of 16 x 16, 128 values of the contraction, with a scale
 // of 2^e for each row and column).  A row of Q is scaled by a power of two to at most 448 and split: its nearest code,
 // 16 times what is left of it as a code, and so on.  A code has 4 significant bits and a rest at most half a step of
-// the code before, so two codes hold a bf16 (8 bits) without rounding, as far as it is
-// above 2^-18 of the row's largest: fp32 sums round more.  The scales put the parts back in their places.  Two parts take
+// the code before, so two codes hold a bf16 (8 bits) without rounding where the first is a normal code: from 2^-13.8 of the row's
+// largest value on (2^-6 of 225).  Below that the second code's grid, 2^-9 / 16, rounds: by 2^-14 of 225 at most, 2^-21.8 of the
+// row's largest -- what fp32 sums of products with that value round by too, but in a row whose score does not hold
+// that product (K is zero there) it is the row's error.  The scales put the parts back in their places.  Two parts take
 // as long as the bf16 product of widened codes, without the widening and with half the bytes to read.  (A half has 11 bits: three
 // codes, half as long again, and more registers than there are; there K is widened.  1024 tokens on 30720 keys, 64/8 heads, fp16: three
 // codes 1016 us, K widened 924; 8 chunks of 2000-2600 on up to 4096, 32/8, 755 and 701.)

@@ -627,3 +627,33 @@ def test_what_an_infinity_becomes(new):
         assert np.array_equal(V, want)
         want[-1, 0, 9] = -value
         assert np.array_equal(K, want)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,above", [(torch.bfloat16, 2.0 ** 4), (torch.bfloat16, 2.0 ** 12), (torch.bfloat16, 2.0 ** 15), (torch.bfloat16, 2.0 ** 17),
+                                         (torch.float16, 2.0 ** 4), (torch.float16, 2.0 ** 12)])
+def test_a_feature_of_q_far_above_the_others_where_k_is_zero(above, D, dtype):
+    """The scores come from the small values alone.  Under bf16 a chunk's Q is two codes a value: 2^-21.8 of the row's largest may be
+    missing from each, top * 2^-21.8 * sum |K_j| from a score; an error of d in the exponents makes at most e^(2d) - 1 of a
+    weight.  (fp16 ends at 65504.)"""
+    w = filled([300, 9], [40, 33], 2, D, 54, dtype)
+    G, far = 3, 11
+    for page in range(w.P):
+        for h in range(2):
+            codes, _ = kv8.block(w.pool, 0, page, 0, h, 2, D)
+            codes[kv8.k_index(np.arange(16), far)] = 0
+    q = queries(w, G)
+    q[:, :, far] *= above
+    got, qf, h16, scale = attend(w, G, q).double().cpu().numpy(), q.double().cpu().numpy(), HALF_STEP[dtype], 1.0 / np.sqrt(D)
+    for s in range(2):
+        c, n, t0 = w.ctx[s], w.new[s], int(w.cu[s])
+        K, V = kv8.read_logical(w.pool, 0, w.tables[s], c + n, 2, D)
+        ref, spread, reach = kv8.attention(qf[t0:t0 + n], K, V, c, scale)
+        top = np.abs(qf[t0:t0 + n]).max(-1)
+        most = np.repeat(np.abs(K).sum(-1).max(0), G)                    # of a kv head's keys
+        off = scale * top * 2.0 ** -21.8 * most[None] if dtype == torch.bfloat16 else 0.0 * top
+        fold = h16 if dtype == torch.float16 else 0.0
+        weights = 1.01 * (h16 + np.expm1(2 * (off + (fold + 2.0 ** -20) * reach)))[..., None] * spread
+        tiny = (c + n) * 2.0 ** -25 * 2 * np.abs(V).max() if dtype == torch.float16 else 0.0
+        bound = 1.01 * (h16 + 2.0 ** -20) * np.abs(ref) + weights + tiny + 2.0 ** -20 * np.abs(V).max()
+        assert (np.abs(got[t0:t0 + n] - ref) <= bound).all()
