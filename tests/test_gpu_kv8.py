@@ -657,3 +657,25 @@ def test_a_feature_of_q_far_above_the_others_where_k_is_zero(above, D, dtype):
         tiny = (c + n) * 2.0 ** -25 * 2 * np.abs(V).max() if dtype == torch.float16 else 0.0
         bound = 1.01 * (h16 + 2.0 ** -20) * np.abs(ref) + weights + tiny + 2.0 ** -20 * np.abs(V).max()
         assert (np.abs(got[t0:t0 + n] - ref) <= bound).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_half_precision_blocks_of_very_small_values(D):
+    """fp16 values down to its subnormal ones, 2^-24, in pages of different scales, in decodes and chunks: the codes of such a value are
+    multiples of 2^-24, so widening them to half precision rounds nothing."""
+    w = World([0, 0], [160, 160], 2, D, 55, torch.float16)
+    k, v = w.rows(w.T), w.rows(w.T)
+    for p in range(20):
+        v[p * 16:(p + 1) * 16] *= 2.0 ** -(p % 10 + 8)
+        k[p * 16:(p + 1) * 16] *= 2.0 ** -(p % 7 + 8)
+    k, v = (torch.from_numpy(x).half().double().numpy() for x in (k, v))
+    kv8.ref_append(w.pool, 0, w.tables, [0, 0], w.cu, k, v, 2, D, True)
+    for s in range(2):
+        for x in kv8.read_logical(w.pool, 0, w.tables[s], 160, 2, D):
+            assert np.array_equal(x, x.astype(np.float16)) and (np.abs(x[x != 0]) < 2.0 ** -14).any()
+    q = queries(w, 4, 2.0 ** 9)
+    check_attention(w, 4, attend(w, 4, q), q)
+    d = World([159, 159], [1, 1], 2, D, 55, torch.float16)               # the last of either as decodes
+    d.pool, d.tables, d.P = w.pool, w.tables, w.P
+    qd = q[[159, 319]].contiguous()
+    check_attention(d, 4, attend(d, 4, qd), qd)
