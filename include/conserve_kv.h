@@ -541,7 +541,8 @@ void cs_set_decode_pages_ahead(int32_t pages);
  * tokens can run as two kernels in a row, as one grid with the decode work behind the tiles, or
  * as one grid with one decode workgroup per CU beside the tiles (paper Sec. 4.2: both kinds of
  * work share an iteration).  1 (default): the host chooses from the batch's lengths; 0: always
- * two kernels; 2: always behind; 3: always beside.  All give the same bits.  Process-wide. */
+ * two kernels; 2: always behind; 3: always beside.  All give the same bits where they cut the same tiles (the host may cut them
+ * otherwise in one grid than in a grid of their own: then sums are rounded in another order).  Process-wide. */
 void cs_set_mixed_fusion(int32_t mode);
 
 /* Host-only view of that choice, for tests: 0 two kernels (also when the batch has only one kind
@@ -565,6 +566,10 @@ int32_t cs_debug_mixed_tile_priority(const cs_batch* batch, int32_t num_q_heads,
  * has 0 slots and 1 range).  CS_ERR_INVALID_ARG on bad arguments.  No device work. */
 int32_t cs_debug_mixed_tail_cut(const cs_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                 int32_t* first_cut, int32_t* ranges);
+
+/* The same two views of a batch over an 8-bit pool: returns the arrangement (as cs_debug_mixed_arrangement), *ranges the ranges of the
+ * longest cut tile (1: nothing is cut). */
+int32_t cs_debug_mixed_kv8(const cs_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t* ranges);
 
 /* The host's model of a fused grid's tile workgroups, for tests (no device work): n workgroups
  * that take work_us[i] microseconds each beside another tile, 0.78 of that alone on their CU

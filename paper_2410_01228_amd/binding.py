@@ -176,6 +176,7 @@ def lib():
         L.cs_debug_copy.restype, L.cs_debug_copy.argtypes = ctypes.c_int, [vp, vp, sz, vp]
         L.cs_set_decode_split_tokens.restype, L.cs_set_decode_split_tokens.argtypes = None, [i32]
         L.cs_set_mixed_fusion.restype, L.cs_set_mixed_fusion.argtypes = None, [i32]
+        L.cs_debug_mixed_kv8.restype, L.cs_debug_mixed_kv8.argtypes = i32, [BP, i32, i32, i32, ip]
         L.cs_debug_mixed_arrangement.restype, L.cs_debug_mixed_arrangement.argtypes = i32, [BP, i32, i32, i32]
         L.cs_debug_mixed_tile_priority.restype, L.cs_debug_mixed_tile_priority.argtypes = i32, [BP, i32, i32, i32]
         L.cs_debug_set_tail_cut.restype, L.cs_debug_set_tail_cut.argtypes = None, [i32, i32]
@@ -206,7 +207,7 @@ EXPORTS = [
     "cs_kv8_page_bytes", "cs_kv8_append", "cs_kv8_append_f16", "cs_paged_attention_kv8_workspace_bytes", "cs_paged_attention_mixed_kv8",
     "cs_paged_attention_mixed_kv8_f16", "cs_kv_page_space", "cs_kv8_page_space", "cs_kv_pages_copy", "cs_kv_pages_fork", "cs_kv_pages_free",
     "cs_kv_pages_compact", "cs_kv_pages_compact_workspace_bytes", "cs_debug_set_cu_count", "cs_debug_copy", "cs_debug_decode_items", "cs_debug_decode_pages_ahead", "cs_debug_decode_loads", "cs_debug_prefill_order",
-    "cs_set_decode_split_tokens", "cs_set_decode_pages_ahead", "cs_set_mixed_fusion", "cs_debug_mixed_arrangement", "cs_debug_mixed_tile_priority", "cs_debug_mixed_tail_cut", "cs_debug_set_tail_cut", "cs_debug_play_tiles", "cs_status_string", "cs_last_hip_error",
+    "cs_set_decode_split_tokens", "cs_set_decode_pages_ahead", "cs_set_mixed_fusion", "cs_debug_mixed_arrangement", "cs_debug_mixed_kv8", "cs_debug_mixed_tile_priority", "cs_debug_mixed_tail_cut", "cs_debug_set_tail_cut", "cs_debug_play_tiles", "cs_status_string", "cs_last_hip_error",
 ]
 
 
@@ -686,6 +687,15 @@ def cs_debug_mixed_arrangement(batch: "Batch", Hq: int, Hkv: int, D: int) -> int
     if rc < 0:
         raise CsError(rc, "cs_debug_mixed_arrangement")
     return rc
+
+
+def cs_debug_mixed_kv8(batch: "Batch", Hq: int, Hkv: int, D: int):
+    """(arrangement as above, ranges of the longest cut tile) of a batch over an 8-bit pool -- host only."""
+    ranges = ctypes.c_int32(0)
+    rc = lib().cs_debug_mixed_kv8(ctypes.byref(batch.c), Hq, Hkv, D, ctypes.byref(ranges))
+    if rc < 0:
+        raise CsError(rc, "cs_debug_mixed_kv8")
+    return rc, ranges.value
 
 
 def cs_debug_mixed_tile_priority(batch: "Batch", Hq: int, Hkv: int, D: int) -> int:

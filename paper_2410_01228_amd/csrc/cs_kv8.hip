@@ -457,6 +457,15 @@ int cs_paged_attention_mixed_kv8_f16(const cs_kv8_pool* pool, int32_t layer, con
     return attention_kv8(pool, layer, batch, q, out, Hq, softmax_scale, workspace, workspace_bytes, stream, true);
 }
 
+int32_t cs_debug_mixed_kv8(const cs_batch* batch, int32_t Hq, int32_t Hkv, int32_t D, int32_t* ranges) {
+    if (attention_shape_ok(Hq, Hkv, D) != CS_OK) return CS_ERR_INVALID_ARG;
+    if (validate_batch(nullptr, batch) != CS_OK || batch->num_seqs == 0) return CS_ERR_INVALID_ARG;
+    const Plans* plans = plans8(batch, Hq, Hkv, D);
+    if (!plans) return hip_failed(hipErrorOutOfMemory, "launch plan");
+    if (ranges) *ranges = std::max(plans->p.max_ranges, 1);
+    return plans->f.arrangement;
+}
+
 int cs_kv8_page_space(const cs_kv8_pool* pool, cs_page_space* space) {
     const int rc = validate_kv8(pool);
     if (rc) return rc;

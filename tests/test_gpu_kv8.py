@@ -679,3 +679,49 @@ def test_half_precision_blocks_of_very_small_values(D):
     d.pool, d.tables, d.P = w.pool, w.tables, w.P
     qd = q[[159, 319]].contiguous()
     check_attention(d, 4, attend(d, 4, qd), qd)
+
+
+@pytest.mark.parametrize("which,dtype", [(0, torch.bfloat16), (1, torch.float16), (1, torch.bfloat16), (2, torch.bfloat16), (2, torch.float16)])
+def test_mixes_at_model_shapes_run_as_planned_and_are_right_in_every_part_of_a_chunk(which, dtype):
+    """The arrangement is asked for first (tiles whole with decode work behind them; two kernels; cut tiles): then rows of the
+    first, a middle and the last tile of each chunk against the oracle."""
+    from test_kv8_host import ARRANGED, arranged_batch
+    Hq, Hkv, decodes, chunks, want = ARRANGED[which]
+    ctx, new = arranged_batch(decodes, chunks)
+    w = drawn_pool(ctx, new, Hkv, 128, 56, dtype)
+    q = queries(w, Hq // Hkv)
+    try:
+        cs.cs_debug_set_cu_count(256)
+        assert cs.cs_debug_mixed_kv8(w.batch(), Hq, Hkv, 128) == want
+        out = attend(w, Hq // Hkv, q)
+    finally:
+        cs.cs_debug_set_cu_count(0)
+    assert torch.isfinite(out.float()).all()
+    check_attention(w, Hq // Hkv, out, q, seqs=[1, decodes[0] // 3])
+    for s in range(decodes[0], len(ctx)):
+        for t in (0, new[s] // 2 - 1, new[s] - 3):
+            part = types.SimpleNamespace(Hkv=Hkv, D=128, dtype=dtype, pool=w.pool, layer=0, tables=w.tables[s:s + 1], ctx=[ctx[s] + t], new=[3], cu=np.array([0, 3]))
+            rows = slice(int(w.cu[s]) + t, int(w.cu[s]) + t + 3)
+            check_attention(part, Hq // Hkv, out[rows], q[rows])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("Hq,Hkv,decodes,chunks", [(32, 8, (100, 100, 3000), [(2000, 300), (50, 700)]), (4, 2, (64, 1000, 8000), [(5000, 512)])])
+def test_mixes_of_head_dim_64_at_model_sizes(Hq, Hkv, decodes, chunks, dtype):
+    from test_kv8_host import arranged_batch
+    ctx, new = arranged_batch(decodes, chunks)
+    w = drawn_pool(ctx, new, Hkv, 64, 57, dtype)
+    q = queries(w, Hq // Hkv)
+    for mode in (0, 2, 3):
+        try:
+            cs.cs_set_mixed_fusion(mode)
+            out = attend(w, Hq // Hkv, q)
+        finally:
+            cs.cs_set_mixed_fusion(1)
+        assert torch.isfinite(out.float()).all()
+        check_attention(w, Hq // Hkv, out, q, seqs=[0, decodes[0] - 1])
+        for s in range(decodes[0], len(ctx)):
+            for t in (0, new[s] // 2, new[s] - 3):
+                part = types.SimpleNamespace(Hkv=Hkv, D=64, dtype=dtype, pool=w.pool, layer=0, tables=w.tables[s:s + 1], ctx=[ctx[s] + t], new=[3], cu=np.array([0, 3]))
+                rows = slice(int(w.cu[s]) + t, int(w.cu[s]) + t + 3)
+                check_attention(part, Hq // Hkv, out[rows], q[rows])

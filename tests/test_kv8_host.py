@@ -263,3 +263,37 @@ def test_the_binding_refuses_views_that_the_kernels_would_read_past():
                     attend(pool, 0, b, k, v, 2, 0.125, None, stream=0)
     with pytest.raises(AssertionError):
         cs.Pool8(torch.zeros((3, 2 * cs.cs_kv8_page_bytes(2, 64)), dtype=torch.uint8)[:, ::2], 1, 3, 2, 64)
+
+
+#: Query heads, kv heads, (decodes, their shortest and longest context), chunks as (context, tokens), and what a chip of 256 CUs does
+#: with them: the arrangement (0 two kernels, 1 decode behind the tiles, 2 beside) and the ranges of the longest cut tile.
+ARRANGED = [
+    (28, 4, (64, 1024, 8192), [(3276, 512), (9712, 512), (10901, 512), (6220, 512)], (1, 1)),     # whole, though a grid of their own would cut them
+    (40, 8, (10, 239, 956), [(6461, 576), (768, 861), (232, 761), (3545, 984)], (0, 1)),
+    (64, 8, (60, 500, 2000), [(3000, 300)], (1, 4)),
+    (64, 8, (128, 2048, 32768), [(30720, 1024)], (2, 3)),
+    (32, 8, (200, 1000, 6000), [(4000, 200)], (1, 1)),
+]
+
+
+def arranged_batch(decodes, chunks):
+    r = np.random.default_rng(40)
+    n, lo, hi = decodes
+    return [int(x) for x in r.integers(lo, hi, n)] + [c for c, _ in chunks], [1] * n + [q for _, q in chunks]
+
+
+@pytest.mark.parametrize("Hq,Hkv,decodes,chunks,want", ARRANGED)
+def test_arrangements_of_8_bit_mixes(Hq, Hkv, decodes, chunks, want):
+    b = host_batch(*arranged_batch(decodes, chunks))
+    try:
+        cs.cs_debug_set_cu_count(256)
+        assert cs.cs_debug_mixed_kv8(b, Hq, Hkv, 128) == want
+        for mode, forced in ((0, 0), (2, 1), (3, 2)):
+            cs.cs_set_mixed_fusion(mode)
+            assert cs.cs_debug_mixed_kv8(b, Hq, Hkv, 128)[0] == forced
+    finally:
+        cs.cs_set_mixed_fusion(1)
+        cs.cs_debug_set_cu_count(0)
+    with pytest.raises(cs.CsError):
+        cs.cs_debug_mixed_kv8(b, Hq, 3, 128)
+    assert cs.lib().cs_debug_mixed_kv8(ctypes.byref(b.c), Hq, Hkv, 128, None) in (0, 1, 2)
