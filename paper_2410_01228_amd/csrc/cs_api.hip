@@ -181,8 +181,8 @@ DecodePlan plan_decode(const cs_batch* b, int32_t Hkv, int32_t head_dim, int32_t
         // per CU (over 171 random batches of three shapes: mean distance to the best forced plan
         // 3.8% -> 2.3%, worst 61% -> 17%, together with the floor rule below).
         // (the workgroup counts and byte volumes below were measured on 256 CUs and scale with the chip)
-        // 8-bit pools: items of 8192 keys at either head dim (128 decodes of 2K-32K keys, 64/8 heads, 768 -> 751 us, now 733), everything
-        // else as for the same keys in 16 bits (64 of 1K-8K, 28/4: pieces of 1024 instead of 2048, 61.3 -> 58.8).
+        // 8-bit pools: items of 8192 keys at either head dim (128 decodes of 2K-32K keys, 64/8 heads, 734.7 us, 751.4 with 4096), everything
+        // else as for the same keys in 16 bits (64 of 1K-8K, 28/4, 57.7, by the bytes of 8-bit K and V 59.8; 256 of 1000-8000, 4/2, 57.9 and 60.6).
         const int32_t cap = head_dim >= 128 && elem_bytes == 2 ? 4096 : 8192;
         const int64_t kv_bytes = p.decode_keys * 2 * Hkv * head_dim * 2;
         const int64_t need = p.uniform ? cus : kv_bytes >= 400000000ll * cus / 256 ? 3 * cus : cus * 3 / 2;

@@ -140,10 +140,9 @@ __device__ __forceinline__ void pair_of8(int32_t w, int32_t Hkv, int32_t n_items
 //
 // One form for every launch: a step ahead, with loads that the compiler can count (Loads::kLone there).  A workgroup
 // takes half as long as over 16-bit pages, so more of a launch is the time of its last ones, alone on their CUs, and full chips
-// do not mind (figures from before pair_of8, which took 1-27% off either side): skipped loads, one step ahead, 256 decodes of 512-4096 keys, 32/8 heads, 194.6 us, this 192.3; of 1000-8000, 4/2
-// heads, 90 and 64; 8 of 128-2048 uncut, 32/8, 24.9 and 18.0.  Two steps ahead are within 0.3% on full chips, up to 8% faster for a
-// few long items (1 of 20000, 64/8, pieces of 1024: 18.5 us instead of 19.9) and 1-18% slower for many short ones (300 of
-// 50-500: 48.7 instead of 41.2).  Four workgroups a CU, in 128 registers, spill: 244 us.
+// do not mind.  This, skipped loads, two steps ahead, us: 256 decodes of 512-4096 keys, 32/8 heads, 187.6, 189.4, 192.2; of 1000-8000,
+// 4/2 heads, 57.9, 58.7, 63.7; 300 of 50-500, 64/8, 33.7, 37.0, 43.4; 1 of 20000, 64/8, 20.1, 22.4, 21.4; 128 of 2K-32K beside a chunk of
+// 1024 on 30720, 64/8, 1492, 1621, 1508.  (Four workgroups a CU would have 128 registers each, and spill.)
 template <int D, class Src, class E>
 __device__ __forceinline__ void decode_item8(
     DecodeLds<D>& lds,
