@@ -3,7 +3,8 @@
  * online/offline LLM co-serving: KV append, paged attention over a mixed batch of decode
  * and chunked-prefill tokens, and the gather / restore copies of incremental KV
  * checkpointing (paper Sec. 4.2, 4.3, 4.4, 5); the first two over a cache of 8-bit codes
- * too, and the copies, forks, frees and compaction of whole pages of either.
+ * too, and the copies, forks, frees and compaction of whole pages of either; the norm and rotation
+ * of Q and K on the way there, and the attention, verification and commit of drafted trees.
  *
  * Conventions for every call
  *   - returns a cs_status (0 = CS_OK, negative = error); all checks that need only host
@@ -482,6 +483,100 @@ int cs_kv_pages_compact(const cs_page_space* space, int32_t layer_begin, int32_t
                         const cs_page_tables* tables, const cs_page_tables* new_tables,
                         int32_t* new_ids, int32_t* num_used,
                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Q and K on the way from the projection: norm of each head, rotation ----
+ * A row x of D features becomes, in fp32, rounded once at the end:
+ *   y = x * w / sqrt(mean(x^2) + eps)      with a norm's weights w; else y = x
+ *   pair i < rotary_dim / 2 of y, (a, b), turns by t = position * inv_freq[i]:
+ *   (a cos t - b sin t, b cos t + a sin t)
+ * A pair is features i and i + rotary_dim / 2, or (interleaved) 2 i and 2 i + 1; features from rotary_dim on stay as they
+ * are (normed).  Positions of several axes (time, height, width of an image's or video's token): the first
+ * axis_pairs[0] pairs turn by row 0 of `positions`, the next axis_pairs[1] by row 1, and so on.  Angles are
+ * reduced in fp64, so far positions lose nothing. */
+typedef struct {
+    const float*   inv_freq;        /* device [rotary_dim / 2]; radians a position       */
+    int32_t        rotary_dim;      /* 0 (no rotation) to head_dim, multiple of 8        */
+    int32_t        interleaved;     /* nonzero: pairs are neighbours                     */
+    const int32_t* positions;       /* device [num_axes][num_tokens]; NULL (cs_kv_append_rope, one axis):
+                                       ctx_lens[s] + i                                   */
+    int64_t        position_stride; /* elements from one axis to the next, >= num_tokens (one axis: any) */
+    int32_t        num_axes;        /* 1 to 3                                            */
+    int32_t        axis_pairs[3];   /* their sum is rotary_dim / 2 (one axis: not read)  */
+    const void*    q_norm;          /* device [head_dim], the data's type, 8-byte aligned; NULL: Q is not normed */
+    const void*    k_norm;          /* the same for K                                    */
+    float          eps;             /* >= 0                                              */
+} cs_rope;
+
+/* q_out[t][h] and k_out[t][h], device [T][H][D] (bf16; fp16 in the _f16 call), of rows q + t * q_stride + h * D and k + t * k_stride
+ * + h * D: strides in elements, multiples of 8, at least H * D, so that q and k may be parts of a fused projection's
+ * rows.  All pointers are 16-byte aligned.  An output may be its own input (stride H * D then); else nothing overlaps.
+ * num_q_heads is a multiple of num_kv_heads, head_dim 64 or 128.  num_tokens == 0 is a no-op. */
+int cs_qk_rope(const cs_rope* rope, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+               const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, void* k_out, void* stream);
+int cs_qk_rope_f16(const cs_rope* rope, int32_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                   const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, void* k_out, void* stream);
+
+/* cs_qk_rope and cs_kv_append in one pass: q_out as there, the rotated K and v_new (as it is; rows v_new + t * v_stride + h * D)
+ * appended as cs_kv_append does.  16-bit pools (an 8-bit one takes cs_qk_rope's rows through cs_kv8_append).  T == 0 is a no-op. */
+int cs_kv_append_rope(const cs_kv_pool* pool, int32_t layer, const cs_batch* batch, const cs_rope* rope, int32_t num_q_heads,
+                      const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                      void* q_out, void* stream);
+int cs_kv_append_rope_f16(const cs_kv_pool* pool, int32_t layer, const cs_batch* batch, const cs_rope* rope, int32_t num_q_heads,
+                          const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                          void* q_out, void* stream);
+
+/* ---- Drafted trees (speculative decoding) ----
+ * A sequence's new tokens of a step are the nodes of a tree: node 0 is the last token that is known to stand, every other node
+ * continues a node before it.  The step appends all of them (node i in slot ctx_lens[s] + i, rotated by the position of its
+ * depth), runs them through the layers with cs_paged_attention_tree, holds the drafts against the model's own distributions
+ * with cs_spec_verify, and moves the accepted nodes' K and V together with cs_kv_tree_commit; the next step's
+ * ctx_lens[s] is count[s] larger. */
+#define CS_MAX_TREE 256             /* nodes of a sequence at most */
+#define CS_MAX_VOCAB (1 << 20)
+
+/* Attention of one layer: node i of sequence s sees its ctx_lens[s] cached tokens and those nodes j of its own sequence whose bit j % 64
+ * is set in tree_mask[cu_q_lens[s] + i][j / 64]; tree_mask: device [T][mask_words], mask_words >= ceil(nodes / 64) and at most
+ * CS_MAX_TREE / 64; NULL: nodes 0 .. i (a chain).  Any mask will do; a row that sees no key at all is zeros.  What lies
+ * in K or V of a key that a row does not see has no effect on it, infinities and NaN among it.  Bits of nodes that the
+ * sequence does not have are not looked at.  Everything else is as in cs_paged_attention_mixed (a single token is a tree of
+ * one node); chunks of more than CS_MAX_TREE tokens are CS_ERR_UNSUPPORTED.  workspace: at least
+ * cs_paged_attention_tree_workspace_bytes(), 0 for many batches; contents are scratch, and calls that overlap in
+ * time need one each. */
+size_t cs_paged_attention_tree_workspace_bytes(const cs_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim);
+int cs_paged_attention_tree(const cs_kv_pool* pool, int32_t layer, const cs_batch* batch, const void* q, void* out,
+                            int32_t num_q_heads, float softmax_scale, const uint64_t* tree_mask, int32_t mask_words,
+                            void* workspace, size_t workspace_bytes, void* stream);
+int cs_paged_attention_tree_f16(const cs_kv_pool* pool, int32_t layer, const cs_batch* batch, const void* q, void* out,
+                                int32_t num_q_heads, float softmax_scale, const uint64_t* tree_mask, int32_t mask_words,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Verification.  For every sequence, from node n = 0 on: R = p[n], Z = 1, and n's children are tried in ascending order.
+ * Child i with token x = tokens[i] is accepted if
+ *     q given (drafts drawn from rows of q):  u[i] * q[n][x] * Z < R[x]; else R = max(p[n] - c q[n], 0) with c the sum of the Z so
+ *                                             far, and Z = sum R: the distribution max(R / Z - q, 0), not normalised
+ *     q NULL (fixed guesses):                 u[i] * Z < R[x]; else Z = Z - R[x], R[x] = 0
+ * and the walk goes on from it; where no child is accepted, or there is none, the token that follows is the first one at which the running sum of
+ * R passes u_next[s] * sum R.  With u, u_next uniform on [0, 1) the tokens are distributed as p's own.  All decisions in
+ * fp64.  Where nothing is left of R it is p[n] that is drawn from; where there is nothing either, the token is -1.  An element that is negative
+ * or no number counts as 0; a token outside the vocabulary is refused.
+ *   tokens, parents, u: device [T], entries of node 0 not read; parents[i] < i, in the sequence's own numbers (a node whose parent
+ *   is none of 0 .. i - 1 is never reached), NULL: a chain.  p, q: device fp32, the row of token t from p + t * p_stride on
+ *   (strides in elements, >= vocab); the distribution behind t, and the one that t's children were drawn from.
+ *   u_next: device [S].
+ *   out_tokens[cu_q_lens[s] + k]: the tokens that the step brings, k < count[s], then -1;  path[..]: their nodes' numbers, node 0 first
+ *   (token k follows node path[k]), then -1;  count: device [S], accepted drafts + 1; 0 for a sequence without new tokens.
+ * Of `batch` only num_seqs, num_tokens and cu_q_lens are used beyond its checks.  workspace: device, 16-byte aligned, as asked
+ * for the batch's num_seqs; contents are scratch, and calls that overlap in time need one each. */
+size_t cs_spec_verify_workspace_bytes(int32_t num_seqs, int32_t vocab);
+int cs_spec_verify(const cs_batch* batch, int32_t vocab, const int32_t* tokens, const int32_t* parents,
+                   const float* p, int64_t p_stride, const float* q, int64_t q_stride, const float* u, const float* u_next,
+                   int32_t* out_tokens, int32_t* path, int32_t* count, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Commit: K and V of node path[cu_q_lens[s] + k] go to slot ctx_lens[s] + k, k < count[s], in layers layer_begin .. layer_end - 1; no
+ * other slot changes.  path and count as cs_spec_verify leaves them: a path ascends.  batch: the step's, with the lengths
+ * from before it.  A node outside the sequence's, or in a page outside the pool, is skipped. */
+int cs_kv_tree_commit(const cs_kv_pool* pool, int32_t layer_begin, int32_t layer_end, const cs_batch* batch,
+                      const int32_t* path, const int32_t* count, void* stream);
 
 /* Plain device-to-device copy kernel of `bytes` (multiple of 16, both pointers 16-byte
  * aligned): the measured copy ceiling of the device and the calibration point for hardware

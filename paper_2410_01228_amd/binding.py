@@ -103,6 +103,21 @@ class cs_page_tables(ctypes.Structure):
     ]
 
 
+class cs_rope(ctypes.Structure):
+    _fields_ = [
+        ("inv_freq", ctypes.c_void_p),
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("positions", ctypes.c_void_p),
+        ("position_stride", ctypes.c_int64),
+        ("num_axes", ctypes.c_int32),
+        ("axis_pairs", ctypes.c_int32 * 3),
+        ("q_norm", ctypes.c_void_p),
+        ("k_norm", ctypes.c_void_p),
+        ("eps", ctypes.c_float),
+    ]
+
+
 class CsError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -172,6 +187,18 @@ def lib():
         L.cs_kv_pages_free.restype, L.cs_kv_pages_free.argtypes = ctypes.c_int, [TP, vp, i32, vp, vp, vp]
         L.cs_kv_pages_compact_workspace_bytes.restype, L.cs_kv_pages_compact_workspace_bytes.argtypes = sz, [i32]
         L.cs_kv_pages_compact.restype, L.cs_kv_pages_compact.argtypes = ctypes.c_int, [SP, i32, i32, TP, TP, vp, vp, vp, sz, vp]
+        RP, i64 = ctypes.POINTER(cs_rope), ctypes.c_int64
+        for f in (L.cs_qk_rope, L.cs_qk_rope_f16):
+            f.restype, f.argtypes = ctypes.c_int, [RP, i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp]
+        for f in (L.cs_kv_append_rope, L.cs_kv_append_rope_f16):
+            f.restype, f.argtypes = ctypes.c_int, [PP, i32, BP, RP, i32, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.cs_paged_attention_tree_workspace_bytes.restype = sz
+        L.cs_paged_attention_tree_workspace_bytes.argtypes = [BP, i32, i32, i32]
+        for f in (L.cs_paged_attention_tree, L.cs_paged_attention_tree_f16):
+            f.restype, f.argtypes = ctypes.c_int, [PP, i32, BP, vp, vp, i32, ctypes.c_float, vp, i32, vp, sz, vp]
+        L.cs_spec_verify_workspace_bytes.restype, L.cs_spec_verify_workspace_bytes.argtypes = sz, [i32, i32]
+        L.cs_spec_verify.restype, L.cs_spec_verify.argtypes = ctypes.c_int, [BP, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.cs_kv_tree_commit.restype, L.cs_kv_tree_commit.argtypes = ctypes.c_int, [PP, i32, i32, BP, vp, vp, vp]
         L.cs_debug_set_cu_count.restype, L.cs_debug_set_cu_count.argtypes = None, [i32]
         L.cs_debug_copy.restype, L.cs_debug_copy.argtypes = ctypes.c_int, [vp, vp, sz, vp]
         L.cs_set_decode_split_tokens.restype, L.cs_set_decode_split_tokens.argtypes = None, [i32]
@@ -206,7 +233,9 @@ EXPORTS = [
     "cs_page_map_evict", "cs_page_map_bind", "cs_page_map_drop", "cs_run_layers", "cs_run_layers_f16", "cs_run_layers_workspace_bytes",
     "cs_kv8_page_bytes", "cs_kv8_append", "cs_kv8_append_f16", "cs_paged_attention_kv8_workspace_bytes", "cs_paged_attention_mixed_kv8",
     "cs_paged_attention_mixed_kv8_f16", "cs_kv_page_space", "cs_kv8_page_space", "cs_kv_pages_copy", "cs_kv_pages_fork", "cs_kv_pages_free",
-    "cs_kv_pages_compact", "cs_kv_pages_compact_workspace_bytes", "cs_debug_set_cu_count", "cs_debug_copy", "cs_debug_decode_items", "cs_debug_decode_pages_ahead", "cs_debug_decode_loads", "cs_debug_prefill_order",
+    "cs_kv_pages_compact", "cs_kv_pages_compact_workspace_bytes", "cs_qk_rope", "cs_qk_rope_f16", "cs_kv_append_rope", "cs_kv_append_rope_f16",
+    "cs_paged_attention_tree_workspace_bytes", "cs_paged_attention_tree", "cs_paged_attention_tree_f16", "cs_spec_verify_workspace_bytes", "cs_spec_verify", "cs_kv_tree_commit",
+    "cs_debug_set_cu_count", "cs_debug_copy", "cs_debug_decode_items", "cs_debug_decode_pages_ahead", "cs_debug_decode_loads", "cs_debug_prefill_order",
     "cs_set_decode_split_tokens", "cs_set_decode_pages_ahead", "cs_set_mixed_fusion", "cs_debug_mixed_arrangement", "cs_debug_mixed_kv8", "cs_debug_mixed_tile_priority", "cs_debug_mixed_tail_cut", "cs_debug_set_tail_cut", "cs_debug_play_tiles", "cs_status_string", "cs_last_hip_error",
 ]
 
@@ -637,6 +666,133 @@ def cs_kv_pages_compact(space: PageSpace, layer_begin: int, layer_end: int, tabl
 
 def compact_workspace_for(space: PageSpace, device="cuda") -> torch.Tensor:
     return torch.empty(int(lib().cs_kv_pages_compact_workspace_bytes(space.c.num_pages)), dtype=torch.uint8, device=device)
+
+
+class Rope:
+    """A cs_rope; keeps its tensors alive.  inv_freq: float32 [rotary_dim / 2]; positions: int32 [tokens] or [axes, tokens] (None: the
+    batch's own, for cs_kv_append_rope); axis_pairs: pairs of each axis, where there are several; q_norm, k_norm: weights [head_dim]."""
+
+    def __init__(self, inv_freq: Optional[torch.Tensor], rotary_dim: int, positions: Optional[torch.Tensor] = None, axis_pairs=None, interleaved: bool = False,
+                 q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        if positions is not None and positions.dim() == 1:
+            positions = positions[None]
+        assert inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and 2 * inv_freq.numel() >= rotary_dim)
+        assert positions is None or (positions.dtype == torch.int32 and positions.dim() == 2 and (positions.shape[1] <= 1 or positions.stride(1) == 1))
+        assert all(w is None or (w.is_contiguous() and w.element_size() == 2) for w in (q_norm, k_norm))
+        axes = 1 if positions is None else int(positions.shape[0])
+        assert axes == 1 or len(axis_pairs) == axes
+        self.tensors = (inv_freq, positions, q_norm, k_norm)
+        self.num_positions = None if positions is None else int(positions.shape[1])
+        pairs = (ctypes.c_int32 * 3)(*([int(n) for n in axis_pairs] + [0] * (3 - axes) if axes > 1 else (rotary_dim // 2, 0, 0)))
+        self.c = cs_rope(_ptr(inv_freq), rotary_dim, int(bool(interleaved)), _ptr(positions), 0 if positions is None or axes == 1 else positions.stride(0), axes, pairs,
+                         _ptr(q_norm), _ptr(k_norm), eps)
+
+    def _holds(self, tokens: int, D: int) -> bool:
+        return (self.num_positions is None or self.num_positions >= tokens) and all(w is None or w.numel() >= D for w in self.tensors[2:])
+
+
+def _head_rows(t: torch.Tensor, tokens: int, heads: int, D: int):
+    """(address, elements between tokens) of a [tokens, heads, D] tensor whose tokens may lie apart."""
+    assert t.element_size() == 2 and t.dim() == 3 and t.shape[0] >= tokens and t.shape[1:] == (heads, D) and t.stride()[1:] == (D, 1)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * D
+
+
+def _qk_rope(fn, where, rope: Rope, q, k, q_out, k_out, stream):
+    T, Hq, D = q.shape
+    Hkv = k.shape[1]
+    assert rope._holds(T, D)
+    _check(fn(ctypes.byref(rope.c), T, Hq, Hkv, D, *_head_rows(q, T, Hq, D), *_head_rows(k, T, Hkv, D), _rows(q_out, T * Hq * D), _rows(k_out, T * Hkv * D),
+              _stream(stream)), where)
+
+
+def cs_qk_rope(rope: Rope, q: torch.Tensor, k: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor, stream=None):
+    """q: [T, Hq, D], k: [T, Hkv, D], both possibly parts of wider rows; outputs contiguous."""
+    _qk_rope(lib().cs_qk_rope, "cs_qk_rope", rope, q, k, q_out, k_out, stream)
+
+
+def cs_qk_rope_f16(rope: Rope, q: torch.Tensor, k: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor, stream=None):
+    _qk_rope(lib().cs_qk_rope_f16, "cs_qk_rope_f16", rope, q, k, q_out, k_out, stream)
+
+
+def _append_rope(fn, where, pool: Pool, layer, batch: Batch, rope: Rope, q, k_new, v_new, q_out, stream):
+    T, Hq, D = batch.c.num_tokens, int(q.shape[1]), pool.D
+    assert rope._holds(T, D)
+    _check(fn(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), ctypes.byref(rope.c), Hq, *_head_rows(q, T, Hq, D), *_head_rows(k_new, T, pool.Hkv, D),
+              *_head_rows(v_new, T, pool.Hkv, D), _rows(q_out, T * Hq * D), _stream(stream)), where)
+
+
+def cs_kv_append_rope(pool: Pool, layer: int, batch: Batch, rope: Rope, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, q_out: torch.Tensor,
+                      stream=None):
+    """q: [T, Hq, D], k_new, v_new: [T, Hkv, D], possibly parts of wider rows; q_out contiguous."""
+    _append_rope(lib().cs_kv_append_rope, "cs_kv_append_rope", pool, layer, batch, rope, q, k_new, v_new, q_out, stream)
+
+
+def cs_kv_append_rope_f16(pool: Pool, layer: int, batch: Batch, rope: Rope, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, q_out: torch.Tensor,
+                          stream=None):
+    _append_rope(lib().cs_kv_append_rope_f16, "cs_kv_append_rope_f16", pool, layer, batch, rope, q, k_new, v_new, q_out, stream)
+
+
+def cs_paged_attention_tree_workspace_bytes(batch: Batch, Hq: int, Hkv: int, D: int) -> int:
+    return int(lib().cs_paged_attention_tree_workspace_bytes(ctypes.byref(batch.c), Hq, Hkv, D))
+
+
+def workspace_for_tree(batch: Batch, Hq: int, Hkv: int, D: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(cs_paged_attention_tree_workspace_bytes(batch, Hq, Hkv, D), 16), dtype=torch.uint8, device=device)
+
+
+def _tree(fn, where, pool: Pool, layer, batch: Batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream):
+    n = batch.c.num_tokens * Hq * pool.D
+    words = 0
+    if tree_mask is not None:
+        assert tree_mask.dim() == 2 and tree_mask.element_size() == 8 and tree_mask.is_contiguous() and tree_mask.shape[0] >= batch.c.num_tokens
+        words = int(tree_mask.shape[1])
+    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(fn(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _rows(q, n), _rows(out, n), Hq, softmax_scale, _ptr(tree_mask), words, _ptr(workspace), wb,
+              _stream(stream)), where)
+
+
+def cs_paged_attention_tree(pool: Pool, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor, Hq: int, softmax_scale: float,
+                            tree_mask: Optional[torch.Tensor], workspace: Optional[torch.Tensor], stream=None):
+    """tree_mask: int64 [T, words] (bit j % 64 of word j / 64: node j is seen), or None: chains."""
+    _tree(lib().cs_paged_attention_tree, "cs_paged_attention_tree", pool, layer, batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream)
+
+
+def cs_paged_attention_tree_f16(pool: Pool, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor, Hq: int, softmax_scale: float,
+                                tree_mask: Optional[torch.Tensor], workspace: Optional[torch.Tensor], stream=None):
+    _tree(lib().cs_paged_attention_tree_f16, "cs_paged_attention_tree_f16", pool, layer, batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream)
+
+
+def cs_spec_verify_workspace_bytes(num_seqs: int, vocab: int) -> int:
+    return int(lib().cs_spec_verify_workspace_bytes(num_seqs, vocab))
+
+
+def workspace_for_verify(batch: Batch, vocab: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(cs_spec_verify_workspace_bytes(batch.c.num_seqs, vocab), 16), dtype=torch.uint8, device=device)
+
+
+def _prob_rows(t: torch.Tensor, tokens: int, vocab: int):
+    assert t.dtype is torch.float32 and t.dim() == 2 and t.shape[0] >= tokens and t.shape[1] == vocab and (t.stride(1) == 1 or vocab == 1)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else vocab
+
+
+def _floats(t: torch.Tensor, n: int) -> int:
+    assert t.dtype is torch.float32 and t.is_contiguous() and t.numel() >= n
+    return t.data_ptr()
+
+
+def cs_spec_verify(batch: Batch, tokens: torch.Tensor, parents: Optional[torch.Tensor], p: torch.Tensor, q: Optional[torch.Tensor], u: torch.Tensor,
+                   u_next: torch.Tensor, out_tokens: torch.Tensor, path: torch.Tensor, count: torch.Tensor, workspace: Optional[torch.Tensor], stream=None):
+    """p, q: float32 [T, vocab]; q None: the drafts are fixed guesses; parents None: chains."""
+    T, S, vocab = batch.c.num_tokens, batch.c.num_seqs, int(p.shape[1])
+    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().cs_spec_verify(ctypes.byref(batch.c), vocab, _list(tokens, T), None if parents is None else _list(parents, T), *_prob_rows(p, T, vocab),
+                                *((None, 0) if q is None else _prob_rows(q, T, vocab)), _floats(u, T), _floats(u_next, S), _list(out_tokens, T), _list(path, T),
+                                _list(count, S), _ptr(workspace), wb, _stream(stream)), "cs_spec_verify")
+
+
+def cs_kv_tree_commit(pool: Pool, layer_begin: int, layer_end: int, batch: Batch, path: torch.Tensor, count: torch.Tensor, stream=None):
+    _check(lib().cs_kv_tree_commit(ctypes.byref(pool.c), layer_begin, layer_end, ctypes.byref(batch.c), _list(path, batch.c.num_tokens),
+                                   _list(count, batch.c.num_seqs), _stream(stream)), "cs_kv_tree_commit")
 
 
 def cs_debug_set_cu_count(cus: int):

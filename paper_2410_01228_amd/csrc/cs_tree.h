@@ -1,0 +1,38 @@
+// What the host and the kernels of tree attention share: how a sequence's rows are blocked and its keys are cut.
+#pragma once
+#include "cs_common.h"
+
+namespace cs {
+
+constexpr int kTreeWords = CS_MAX_TREE / 64;                     // mask words of a node at most
+constexpr int kTreeTiles = 4;                                    // column tiles (16 rows) of a workgroup at most
+
+// The column tiles of R = nodes * G rows, dealt evenly to as few workgroups as hold them.
+struct TreeBlocks { int32_t blocks, tiles; };
+__host__ __device__ inline TreeBlocks tree_blocks(int32_t rows) {
+    const int32_t all = (rows + 15) / 16, blocks = (all + kTreeTiles - 1) / kTreeTiles;
+    return {blocks, blocks ? (all + blocks - 1) / blocks : 0};
+}
+
+// Keys of a piece of a sequence of n keys cut into k: whole rounds of the four wavefronts' 32-key steps.
+__host__ __device__ inline int32_t tree_chunk_keys(int32_t n_keys, int32_t pieces) {
+    if (pieces <= 1) return n_keys;
+    return ((n_keys + pieces - 1) / pieces + 127) & ~127;
+}
+
+// A work item in the kernel arguments: sequence (bits 0-15), piece (16-20), pieces - 1 (21-25), block of rows (26-31).
+// (256 nodes of 16 heads: 64 blocks.)
+constexpr int kTreeMaxPieces = 32;
+struct TreeItem { int32_t seq, piece, pieces, block; };
+__host__ __device__ inline TreeItem tree_item(uint32_t w) {
+    return {(int32_t)(w & 0xffffu), (int32_t)(w >> 16 & 31u), (int32_t)(w >> 21 & 31u) + 1, (int32_t)(w >> 26)};
+}
+__host__ __device__ inline uint32_t tree_word(int32_t seq, int32_t piece, int32_t pieces, int32_t block) {
+    return (uint32_t)seq | (uint32_t)piece << 16 | (uint32_t)(pieces - 1) << 21 | (uint32_t)block << 26;
+}
+struct TreeItems {
+    int32_t base;                                                // number of the first item, of all the call's
+    uint32_t e[kMaxArgItems];
+};
+
+}  // namespace cs

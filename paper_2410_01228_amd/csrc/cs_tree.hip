@@ -1,0 +1,170 @@
+// Attention of drafted trees over the paged cache: the launch plan and the C entries (kernels: cs_tree_impl.h).
+#include <algorithm>
+#include <new>
+#include <vector>
+#include "cs_plan.h"
+#include "cs_tree.h"
+#include "cs_tree_impl.h"
+
+namespace cs {
+
+// How a batch is launched: a pure function of the host lengths, the shape and the chip.
+struct TreePlan {
+    int32_t tiles = 0;                                           // column tiles of a workgroup: 1, 2 or 4
+    bool cut = false;                                            // some sequence comes in pieces
+    std::vector<uint32_t> items;                                 // in launch order: a sequence's pieces and, innermost, its blocks stand together
+    std::vector<int32_t> launches;                               // first items of the launches
+    size_t ml_bytes = 0, bytes = 0;                              // workspace: (max, sum) of the partials, all of it
+};
+
+static size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
+
+static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D) {
+    TreePlan p;
+    const int32_t G = Hq / Hkv, S = b->num_seqs;
+    int32_t most = 1;
+    int64_t whole = 0;
+    for (int32_t s = 0; s < S; ++s) {
+        const TreeBlocks t = tree_blocks((b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s]) * G);
+        most = std::max(most, t.tiles);
+        whole += t.blocks;
+    }
+    p.tiles = most <= 1 ? 1 : most <= 2 ? 2 : 4;
+    // Pieces: of 8192 keys, halved until every CU has two workgroups, or down to 512.
+    const int64_t want = 2ll * device_cus();
+    auto pieces_of = [&](int32_t s, int32_t split) {
+        const int32_t q = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s], n = b->h_ctx_lens[s] + q, blocks = tree_blocks(q * G).blocks;
+        if (blocks == 0) return 0;
+        int32_t k = std::min(std::max((n + split / 2) / split, 1), std::min(kTreeMaxPieces, kMaxArgItems / blocks));
+        for (int32_t fewer = k; k > 1; k = fewer) {              // (rounding a piece's length up can leave the last one empty)
+            const int32_t c = tree_chunk_keys(n, k);
+            fewer = (n + c - 1) / c;
+            if (fewer >= k) break;
+        }
+        return k;
+    };
+    int32_t split = 8192;
+    for (; split > 512; split /= 2) {
+        int64_t n = 0;
+        for (int32_t s = 0; s < S; ++s) n += (int64_t)pieces_of(s, split) * tree_blocks((b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s]) * G).blocks;
+        if (n * Hkv >= want) break;
+    }
+    struct Seq { int32_t seq, pieces, blocks, keys; };
+    std::vector<Seq> seqs;
+    seqs.reserve(S);
+    for (int32_t s = 0; s < S; ++s) {
+        const int32_t q = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s], n = b->h_ctx_lens[s] + q, k = pieces_of(s, split);
+        if (k == 0) continue;
+        seqs.push_back({s, k, tree_blocks(q * G).blocks, tree_chunk_keys(n, k)});
+        p.cut = p.cut || k > 1;
+    }
+    std::stable_sort(seqs.begin(), seqs.end(), [](const Seq& x, const Seq& y) { return x.keys > y.keys; });    // the longest first
+    for (const Seq& s : seqs) {
+        if (p.launches.empty() || (int32_t)p.items.size() - p.launches.back() + s.pieces * s.blocks > kMaxArgItems) p.launches.push_back((int32_t)p.items.size());
+        for (int32_t i = 0; i < s.pieces; ++i)
+            for (int32_t k = 0; k < s.blocks; ++k) p.items.push_back(tree_word(s.seq, i, s.pieces, k));
+    }
+    if (p.cut) {
+        const size_t rows = p.items.size() * Hkv * 16 * p.tiles;
+        p.ml_bytes = align16(rows * 2 * sizeof(float));
+        p.bytes = p.ml_bytes + align16(rows * D * sizeof(float));
+    }
+    return p;
+}
+
+template <int D, class E, int PS>
+static void launch_tree(const TreePlan& p, const cs_kv_pool& pool, const uint16_t* layer_base, const cs_batch& b, int32_t G, const uint64_t* mask, int32_t mask_words,
+                        const uint16_t* q, uint16_t* out, float scale_log2e, const TreePartials& part, const TreeItems& items, int32_t n, hipStream_t st) {
+    const dim3 grid((uint32_t)n * (uint32_t)pool.num_kv_heads);
+#define CS_LAUNCH_TREE(NC)                                                                                                          \
+    hipLaunchKernelGGL((tree_kernel<D, E, PS, NC>), grid, dim3(kDecodeThreads), 0, st, layer_base, pool.page_stride, pool.num_pages, \
+                       pool.num_kv_heads, G, b.block_tables, b.max_blocks_per_seq, b.ctx_lens, b.cu_q_lens, mask, mask_words, q, out, scale_log2e, part, items)
+    if (p.tiles == 1) CS_LAUNCH_TREE(1);
+    else if (p.tiles == 2) CS_LAUNCH_TREE(2);
+    else CS_LAUNCH_TREE(4);
+#undef CS_LAUNCH_TREE
+}
+
+template <int D, class E>
+static int run_tree(const TreePlan& p, const cs_kv_pool& pool, int32_t layer, const cs_batch& b, int32_t G, const uint64_t* mask, int32_t mask_words,
+                    const uint16_t* q, uint16_t* out, float scale, void* workspace, hipStream_t st) {
+    const TreePartials part = {p.cut ? (float*)((char*)workspace + p.ml_bytes) : nullptr, p.cut ? (float*)workspace : nullptr};
+    const uint16_t* layer_base = (const uint16_t*)pool.base + (int64_t)layer * pool.layer_stride;
+    for (size_t i = 0; i < p.launches.size(); ++i) {
+        TreeItems items;
+        items.base = p.launches[i];
+        const int32_t end = i + 1 < p.launches.size() ? p.launches[i + 1] : (int32_t)p.items.size(), n = end - items.base;
+        std::copy(p.items.begin() + items.base, p.items.begin() + end, items.e);
+        const float f = scale * 1.44269504088896340736f;
+        if (pool.page_size == 16) launch_tree<D, E, 16>(p, pool, layer_base, b, G, mask, mask_words, q, out, f, part, items, n, st);
+        else                      launch_tree<D, E, 8>(p, pool, layer_base, b, G, mask, mask_words, q, out, f, part, items, n, st);
+        if (p.cut)
+            hipLaunchKernelGGL((tree_merge_kernel<D, E>), dim3((uint32_t)n * (uint32_t)pool.num_kv_heads, (uint32_t)p.tiles), dim3(kDecodeThreads), 0, st,
+                               pool.num_kv_heads, G, 16 * p.tiles, b.cu_q_lens, out, part, items);
+    }
+    return check_launch("tree_kernel");
+}
+
+static int32_t most_new(const cs_batch* b) {
+    int32_t most = 0;
+    for (int32_t s = 0; s < b->num_seqs; ++s) most = std::max(most, b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s]);
+    return most;
+}
+
+static int attention_tree(const cs_kv_pool* pool, int32_t layer, const cs_batch* batch, const void* q, void* out, int32_t Hq, float softmax_scale,
+                          const uint64_t* mask, int32_t mask_words, void* workspace, size_t workspace_bytes, void* stream, bool f16) {
+    int rc = validate_pool(pool);
+    if (rc) return rc;
+    if (layer < 0 || layer >= pool->num_layers) return CS_ERR_INVALID_ARG;
+    const int32_t Hkv = pool->num_kv_heads, D = pool->head_dim;
+    rc = attention_shape_ok(Hq, Hkv, D);
+    if (rc) return rc;
+    rc = validate_batch(pool, batch);
+    if (rc) return rc;
+    if (batch->num_tokens == 0) return CS_OK;
+    const int32_t most = most_new(batch);
+    if (most > CS_MAX_TREE) return CS_ERR_UNSUPPORTED;
+    if (!q || !out || ((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return CS_ERR_INVALID_ARG;
+    if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return CS_ERR_INVALID_ARG;   // positive, finite
+    if (mask && (((uintptr_t)mask & 7) || mask_words < (most + 63) / 64 || mask_words > kTreeWords)) return CS_ERR_INVALID_ARG;
+    try {
+        const TreePlan p = plan_tree(batch, Hq, Hkv, D);
+        if (p.bytes > 0 && (!workspace || ((uintptr_t)workspace & 15))) return CS_ERR_INVALID_ARG;
+        if (workspace_bytes < p.bytes) return CS_ERR_WORKSPACE_TOO_SMALL;
+        const int32_t G = Hq / Hkv;
+        hipStream_t st = (hipStream_t)stream;
+        const uint16_t* qp = (const uint16_t*)q;
+        uint16_t* op = (uint16_t*)out;
+        if (D == 128)
+            return f16 ? run_tree<128, F16>(p, *pool, layer, *batch, G, mask, mask_words, qp, op, softmax_scale, workspace, st)
+                       : run_tree<128, Bf16>(p, *pool, layer, *batch, G, mask, mask_words, qp, op, softmax_scale, workspace, st);
+        return f16 ? run_tree<64, F16>(p, *pool, layer, *batch, G, mask, mask_words, qp, op, softmax_scale, workspace, st)
+                   : run_tree<64, Bf16>(p, *pool, layer, *batch, G, mask, mask_words, qp, op, softmax_scale, workspace, st);
+    } catch (const std::bad_alloc&) {
+        return hip_failed(hipErrorOutOfMemory, "launch plan");
+    }
+}
+
+}  // namespace cs
+
+using namespace cs;
+
+extern "C" {
+
+size_t cs_paged_attention_tree_workspace_bytes(const cs_batch* batch, int32_t Hq, int32_t Hkv, int32_t D) {
+    if (attention_shape_ok(Hq, Hkv, D) != CS_OK) return 0;
+    if (validate_batch(nullptr, batch) != CS_OK || batch->num_seqs == 0 || most_new(batch) > CS_MAX_TREE) return 0;
+    try { return plan_tree(batch, Hq, Hkv, D).bytes; } catch (const std::bad_alloc&) { return 0; }
+}
+
+int cs_paged_attention_tree(const cs_kv_pool* pool, int32_t layer, const cs_batch* batch, const void* q, void* out, int32_t num_q_heads, float softmax_scale,
+                            const uint64_t* tree_mask, int32_t mask_words, void* workspace, size_t workspace_bytes, void* stream) {
+    return attention_tree(pool, layer, batch, q, out, num_q_heads, softmax_scale, tree_mask, mask_words, workspace, workspace_bytes, stream, false);
+}
+
+int cs_paged_attention_tree_f16(const cs_kv_pool* pool, int32_t layer, const cs_batch* batch, const void* q, void* out, int32_t num_q_heads, float softmax_scale,
+                                const uint64_t* tree_mask, int32_t mask_words, void* workspace, size_t workspace_bytes, void* stream) {
+    return attention_tree(pool, layer, batch, q, out, num_q_heads, softmax_scale, tree_mask, mask_words, workspace, workspace_bytes, stream, true);
+}
+
+}  // extern "C"
