@@ -5,7 +5,7 @@
 namespace cs {
 
 constexpr int kTreeWords = CS_MAX_TREE / 64;                     // mask words of a node at most
-constexpr int kTreeTiles = 4;                                    // column tiles (16 rows) of a workgroup at most
+constexpr int kTreeTiles = 8;                                    // column tiles (16 rows) of a workgroup at most
 
 // The column tiles of R = nodes * G rows, dealt evenly to as few workgroups as hold them.
 struct TreeBlocks { int32_t blocks, tiles; };
@@ -21,7 +21,6 @@ __host__ __device__ inline int32_t tree_chunk_keys(int32_t n_keys, int32_t piece
 }
 
 // A work item in the kernel arguments: sequence (bits 0-15), piece (16-20), pieces - 1 (21-25), block of rows (26-31).
-// (256 nodes of 16 heads: 64 blocks.)
 constexpr int kTreeMaxPieces = 32;
 struct TreeItem { int32_t seq, piece, pieces, block; };
 __host__ __device__ inline TreeItem tree_item(uint32_t w) {

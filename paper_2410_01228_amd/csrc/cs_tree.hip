@@ -10,7 +10,7 @@ namespace cs {
 
 // How a batch is launched: a pure function of the host lengths, the shape and the chip.
 struct TreePlan {
-    int32_t tiles = 0;                                           // column tiles of a workgroup: 1, 2 or 4
+    int32_t tiles = 0;                                           // column tiles of a workgroup: 1, 2 (wavefronts share the keys), 4 or 8 (they share the rows)
     bool cut = false;                                            // some sequence comes in pieces
     std::vector<uint32_t> items;                                 // in launch order: a sequence's pieces and, innermost, its blocks stand together
     std::vector<int32_t> launches;                               // first items of the launches
@@ -29,7 +29,7 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
         most = std::max(most, t.tiles);
         whole += t.blocks;
     }
-    p.tiles = most <= 1 ? 1 : most <= 2 ? 2 : 4;
+    p.tiles = most <= 1 ? 1 : most <= 2 ? most : most <= 4 ? 4 : 8;
     // Pieces: of 8192 keys, halved until every CU has two workgroups, or down to 512.
     const int64_t want = 2ll * device_cus();
     auto pieces_of = [&](int32_t s, int32_t split) {
@@ -76,12 +76,13 @@ template <int D, class E, int PS>
 static void launch_tree(const TreePlan& p, const cs_kv_pool& pool, const uint16_t* layer_base, const cs_batch& b, int32_t G, const uint64_t* mask, int32_t mask_words,
                         const uint16_t* q, uint16_t* out, float scale_log2e, const TreePartials& part, const TreeItems& items, int32_t n, hipStream_t st) {
     const dim3 grid((uint32_t)n * (uint32_t)pool.num_kv_heads);
-#define CS_LAUNCH_TREE(NC)                                                                                                          \
-    hipLaunchKernelGGL((tree_kernel<D, E, PS, NC>), grid, dim3(kDecodeThreads), 0, st, layer_base, pool.page_stride, pool.num_pages, \
+#define CS_LAUNCH_TREE(KERNEL, NC)                                                                                                   \
+    hipLaunchKernelGGL((KERNEL<D, E, PS, NC>), grid, dim3(kDecodeThreads), 0, st, layer_base, pool.page_stride, pool.num_pages,        \
                        pool.num_kv_heads, G, b.block_tables, b.max_blocks_per_seq, b.ctx_lens, b.cu_q_lens, mask, mask_words, q, out, scale_log2e, part, items)
-    if (p.tiles == 1) CS_LAUNCH_TREE(1);
-    else if (p.tiles == 2) CS_LAUNCH_TREE(2);
-    else CS_LAUNCH_TREE(4);
+    if (p.tiles == 1) CS_LAUNCH_TREE(tree_kernel, 1);
+    else if (p.tiles == 2) CS_LAUNCH_TREE(tree_kernel, 2);
+    else if (p.tiles == 4) CS_LAUNCH_TREE(tree_ring_kernel, 1);
+    else CS_LAUNCH_TREE(tree_ring_kernel, 2);
 #undef CS_LAUNCH_TREE
 }
 
