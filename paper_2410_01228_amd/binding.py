@@ -682,27 +682,35 @@ class Rope:
         axes = 1 if positions is None else int(positions.shape[0])
         assert axes == 1 or len(axis_pairs) == axes
         self.tensors = (inv_freq, positions, q_norm, k_norm)
-        self.num_positions = None if positions is None else int(positions.shape[1])
+        # how many tokens and features the tensors have entries for
+        self.most_tokens = 2 ** 31 if positions is None else int(positions.shape[1])
+        self.most_features = min([2 ** 31] + [w.numel() for w in (q_norm, k_norm) if w is not None])
         pairs = (ctypes.c_int32 * 3)(*([int(n) for n in axis_pairs] + [0] * (3 - axes) if axes > 1 else (rotary_dim // 2, 0, 0)))
         self.c = cs_rope(_ptr(inv_freq), rotary_dim, int(bool(interleaved)), _ptr(positions), 0 if positions is None or axes == 1 else positions.stride(0), axes, pairs,
                          _ptr(q_norm), _ptr(k_norm), eps)
+        self.ref = ctypes.byref(self.c)
 
-    def _holds(self, tokens: int, D: int) -> bool:
-        return (self.num_positions is None or self.num_positions >= tokens) and all(w is None or w.numel() >= D for w in self.tensors[2:])
+
+_16_BITS = (torch.bfloat16, torch.float16)
 
 
 def _head_rows(t: torch.Tensor, tokens: int, heads: int, D: int):
     """(address, elements between tokens) of a [tokens, heads, D] tensor whose tokens may lie apart."""
-    assert t.element_size() == 2 and t.dim() == 3 and t.shape[0] >= tokens and t.shape[1:] == (heads, D) and t.stride()[1:] == (D, 1)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * D
+    n, h, d = t.shape
+    step, b, c = t.stride()
+    assert n >= tokens and h == heads and d == D == b and c == 1 and t.dtype in _16_BITS
+    return t.data_ptr(), step if n > 1 else h * d
 
 
 def _qk_rope(fn, where, rope: Rope, q, k, q_out, k_out, stream):
     T, Hq, D = q.shape
     Hkv = k.shape[1]
-    assert rope._holds(T, D)
-    _check(fn(ctypes.byref(rope.c), T, Hq, Hkv, D, *_head_rows(q, T, Hq, D), *_head_rows(k, T, Hkv, D), _rows(q_out, T * Hq * D), _rows(k_out, T * Hkv * D),
-              _stream(stream)), where)
+    assert rope.most_tokens >= T and rope.most_features >= D
+    qp, qs = _head_rows(q, T, Hq, D)
+    kp, ks = _head_rows(k, T, Hkv, D)
+    rc = fn(rope.ref, T, Hq, Hkv, D, qp, qs, kp, ks, _rows(q_out, T * Hq * D), _rows(k_out, T * Hkv * D), _stream(stream))
+    if rc:
+        raise CsError(rc, where)
 
 
 def cs_qk_rope(rope: Rope, q: torch.Tensor, k: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor, stream=None):
@@ -715,10 +723,14 @@ def cs_qk_rope_f16(rope: Rope, q: torch.Tensor, k: torch.Tensor, q_out: torch.Te
 
 
 def _append_rope(fn, where, pool: Pool, layer, batch: Batch, rope: Rope, q, k_new, v_new, q_out, stream):
-    T, Hq, D = batch.c.num_tokens, int(q.shape[1]), pool.D
-    assert rope._holds(T, D)
-    _check(fn(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), ctypes.byref(rope.c), Hq, *_head_rows(q, T, Hq, D), *_head_rows(k_new, T, pool.Hkv, D),
-              *_head_rows(v_new, T, pool.Hkv, D), _rows(q_out, T * Hq * D), _stream(stream)), where)
+    T, Hq, Hkv, D = batch.c.num_tokens, q.shape[1], pool.Hkv, pool.D
+    assert rope.most_tokens >= T and rope.most_features >= D
+    qp, qs = _head_rows(q, T, Hq, D)
+    kp, ks = _head_rows(k_new, T, Hkv, D)
+    vp, vs = _head_rows(v_new, T, Hkv, D)
+    rc = fn(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), rope.ref, Hq, qp, qs, kp, ks, vp, vs, _rows(q_out, T * Hq * D), _stream(stream))
+    if rc:
+        raise CsError(rc, where)
 
 
 def cs_kv_append_rope(pool: Pool, layer: int, batch: Batch, rope: Rope, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, q_out: torch.Tensor,
@@ -741,14 +753,16 @@ def workspace_for_tree(batch: Batch, Hq: int, Hkv: int, D: int, device="cuda") -
 
 
 def _tree(fn, where, pool: Pool, layer, batch: Batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream):
-    n = batch.c.num_tokens * Hq * pool.D
-    words = 0
+    T = batch.c.num_tokens
+    n, mask, words = T * Hq * pool.D, None, 0
     if tree_mask is not None:
-        assert tree_mask.dim() == 2 and tree_mask.element_size() == 8 and tree_mask.is_contiguous() and tree_mask.shape[0] >= batch.c.num_tokens
-        words = int(tree_mask.shape[1])
-    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(fn(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _rows(q, n), _rows(out, n), Hq, softmax_scale, _ptr(tree_mask), words, _ptr(workspace), wb,
-              _stream(stream)), where)
+        rows, words = tree_mask.shape
+        assert rows >= T and tree_mask.element_size() == 8 and tree_mask.is_contiguous()
+        mask = tree_mask.data_ptr()
+    ws, wb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    rc = fn(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _rows(q, n), _rows(out, n), Hq, softmax_scale, mask, words, ws, wb, _stream(stream))
+    if rc:
+        raise CsError(rc, where)
 
 
 def cs_paged_attention_tree(pool: Pool, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor, Hq: int, softmax_scale: float,
@@ -771,8 +785,10 @@ def workspace_for_verify(batch: Batch, vocab: int, device="cuda") -> torch.Tenso
 
 
 def _prob_rows(t: torch.Tensor, tokens: int, vocab: int):
-    assert t.dtype is torch.float32 and t.dim() == 2 and t.shape[0] >= tokens and t.shape[1] == vocab and (t.stride(1) == 1 or vocab == 1)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else vocab
+    n, v = t.shape
+    step, one = t.stride()
+    assert n >= tokens and v == vocab and (one == 1 or v == 1) and t.dtype is torch.float32
+    return t.data_ptr(), step if n > 1 else v
 
 
 def _floats(t: torch.Tensor, n: int) -> int:
@@ -783,16 +799,21 @@ def _floats(t: torch.Tensor, n: int) -> int:
 def cs_spec_verify(batch: Batch, tokens: torch.Tensor, parents: Optional[torch.Tensor], p: torch.Tensor, q: Optional[torch.Tensor], u: torch.Tensor,
                    u_next: torch.Tensor, out_tokens: torch.Tensor, path: torch.Tensor, count: torch.Tensor, workspace: Optional[torch.Tensor], stream=None):
     """p, q: float32 [T, vocab]; q None: the drafts are fixed guesses; parents None: chains."""
-    T, S, vocab = batch.c.num_tokens, batch.c.num_seqs, int(p.shape[1])
-    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().cs_spec_verify(ctypes.byref(batch.c), vocab, _list(tokens, T), None if parents is None else _list(parents, T), *_prob_rows(p, T, vocab),
-                                *((None, 0) if q is None else _prob_rows(q, T, vocab)), _floats(u, T), _floats(u_next, S), _list(out_tokens, T), _list(path, T),
-                                _list(count, S), _ptr(workspace), wb, _stream(stream)), "cs_spec_verify")
+    T, S, vocab = batch.c.num_tokens, batch.c.num_seqs, p.shape[1]
+    pp, ps = _prob_rows(p, T, vocab)
+    qp, qs = (None, 0) if q is None else _prob_rows(q, T, vocab)
+    ws, wb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    rc = lib().cs_spec_verify(ctypes.byref(batch.c), vocab, _list(tokens, T), None if parents is None else _list(parents, T), pp, ps, qp, qs, _floats(u, T), _floats(u_next, S),
+                              _list(out_tokens, T), _list(path, T), _list(count, S), ws, wb, _stream(stream))
+    if rc:
+        raise CsError(rc, "cs_spec_verify")
 
 
 def cs_kv_tree_commit(pool: Pool, layer_begin: int, layer_end: int, batch: Batch, path: torch.Tensor, count: torch.Tensor, stream=None):
-    _check(lib().cs_kv_tree_commit(ctypes.byref(pool.c), layer_begin, layer_end, ctypes.byref(batch.c), _list(path, batch.c.num_tokens),
-                                   _list(count, batch.c.num_seqs), _stream(stream)), "cs_kv_tree_commit")
+    rc = lib().cs_kv_tree_commit(ctypes.byref(pool.c), layer_begin, layer_end, ctypes.byref(batch.c), _list(path, batch.c.num_tokens), _list(count, batch.c.num_seqs),
+                                 _stream(stream))
+    if rc:
+        raise CsError(rc, "cs_kv_tree_commit")
 
 
 def cs_debug_set_cu_count(cus: int):

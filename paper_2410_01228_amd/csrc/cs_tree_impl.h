@@ -507,7 +507,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
     // The step's copies have landed, the wavefront's by its own count and the others' by the barrier, behind which nobody reads the step
     // before any more: its slot takes the copies of three steps on.
     auto begin = [&](int32_t i) {
-        const int32_t left = steps - 1 - i;                      // steps behind this one whose copies are under way: 2 at most
+        const int32_t left = min(steps - 1 - i, kTreeRing - 2);  // steps behind this one whose copies are under way
         if (left >= 2) wait_vmcnt<2 * kCopies>();
         else if (left == 1) wait_vmcnt<kCopies>();
         else wait_vmcnt<0>();
