@@ -8,8 +8,11 @@
 // turns: the turns are counted in fp64 (an error of 2^31 / 2 pi * 2^-52, 1e-7 of a turn at most), and what is left of
 // one, at most half, goes on in fp32.
 //
-// HBM-bound: each value is read and written once.  A thread has 8 features of one token, as two pieces of 4 (the two halves of four
-// pairs), and walks heads with the angles in its registers, so that a sine is computed once a token and not once a head.
+// HBM-bound: each value is read and written once.  A thread has 8 features of a row, as two pieces of 4 (the two halves of four pairs).
+// Where rows are written (Q, and K without a cache) a wavefront takes eight heads (16 of head dim 64) of one token, 2 KiB that lie
+// side by side, so that its angles serve two rows of a lane, all of it is one trip to memory, and
+// a launch has wavefronts enough to keep the memory busy (workgroups that walked 16 tokens' heads with the angles computed once ran at
+// half the rate: 10K tokens, 32/8 heads, 96 us).  Where K and V go to a page a workgroup takes its 16 tokens and a few heads.
 #include <algorithm>
 #include "cs_common.h"
 #include "cs_elem.h"
@@ -20,8 +23,8 @@ typedef uint32_t r_u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t r_u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeTokens = 16;                                  // of a workgroup
-constexpr int kRopeRows = 4;                                     // rows of a thread whose loads are in flight together
+constexpr int kRopeTokens = 16;                                  // of a workgroup that fills a page
+constexpr int kRopeRows = 2;                                     // rows of a thread
 
 // What the kernel is told.  Strides in elements.
 struct RopeArgs {
@@ -33,13 +36,14 @@ struct RopeArgs {
     int64_t position_stride;
     float eps;
     int32_t rotary_dim, interleaved, pairs0, pairs1;             // pairs of the first two axes
-    int32_t T, Hq, Hkv, groups;                                  // groups: parts that the heads are dealt in
+    int32_t T, Hq, Hkv;
+    int32_t q_units, kv_units, kv_tokens;                        // wavefronts of a token: with heads of Q; with heads of K, of the tokens in front of kv_tokens
     // the append
     uint16_t* layer_base;
     int64_t page_stride;
     int32_t num_pages, page_size, S, max_blocks;
     const int32_t *block_tables, *ctx_lens, *cu_q_lens;
-    int32_t slot_blocks;                                         // workgroups of sequences with more than one new token
+    int32_t slot_blocks, slot_groups;                            // workgroups of sequences with more than one new token: slots, parts of their heads
 };
 
 // Sum over the 16 (8) lanes that share a row, in each of them.
@@ -60,31 +64,38 @@ struct Turn {
     float c[4], s[4];
 };
 
-template <int D>
-__device__ __forceinline__ Turn turn_of(const RopeArgs& a, int32_t j, int32_t t, int32_t position)
+__device__ __forceinline__ void turn_places(Turn& r, const RopeArgs& a, int32_t j)
 {
-    Turn r;
     r.rotates = 8 * j < a.rotary_dim;
     r.neighbours = a.interleaved != 0 || !r.rotates;
     r.off0 = r.neighbours ? 8 * j : 4 * j;
     r.off1 = r.neighbours ? 8 * j + 4 : a.rotary_dim / 2 + 4 * j;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { r.c[i] = 1.f; r.s[i] = 0.f; }
-    if (r.rotates) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int32_t pair = 4 * j + i;
-            int32_t at = position;
-            if (a.positions) at = a.positions[(pair < a.pairs0 ? 0 : pair < a.pairs1 ? 1 : 2) * a.position_stride + t];
-            const double turns = (double)at * (double)a.inv_freq[pair] * 0.15915494309189535;   // 1 / 2 pi
-            const float part = (float)(turns - rint(turns));
-            sincospif(2.f * part, &r.s[i], &r.c[i]);
-        }
-    }
-    return r;
 }
 
-// One row's 8 features: normed, rotated, rounded.
+__device__ __forceinline__ void turn_angles(Turn& r, const RopeArgs& a, int32_t j, int32_t t, int32_t position)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { r.c[i] = 1.f; r.s[i] = 0.f; }
+    if (!r.rotates) return;
+    int32_t at[4];
+    float freq[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int32_t pair = 4 * j + i;
+        at[i] = position;
+        if (a.positions) at[i] = a.positions[(pair < a.pairs0 ? 0 : pair < a.pairs1 ? 1 : 2) * a.position_stride + t];
+        freq[i] = a.inv_freq[pair];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const double turns = (double)at[i] * (double)freq[i] * 0.15915494309189535;   // 1 / 2 pi
+        const float part = (float)(turns - rint(turns));
+        r.s[i] = __builtin_amdgcn_sinf(part);                    // of a turn: off by 2^-22.9 at most over half a turn (measured at 2^22 points)
+        r.c[i] = __builtin_amdgcn_cosf(part);
+    }
+}
+
+// One row's 8 features: normed, rotated, rounded.  (Every fused multiply-add is spelled out: all kernels round alike.)
 template <int D, class E>
 __device__ __forceinline__ void turn_row(const Turn& r, bool normed, const r_u32x2* w, float eps, r_u32x2& x0, r_u32x2& x1)
 {
@@ -98,8 +109,8 @@ __device__ __forceinline__ void turn_row(const Turn& r, bool normed, const r_u32
     if (normed) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += a[i] * a[i] + b[i] * b[i];
-        const float f = 1.f / sqrtf(row_sum<D / 8>(sum) * (1.f / D) + eps);
+        for (int i = 0; i < 4; ++i) sum = __builtin_fmaf(b[i], b[i], __builtin_fmaf(a[i], a[i], sum));
+        const float f = rsqrtf(__builtin_fmaf(row_sum<D / 8>(sum), 1.f / D, eps));
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             float w0, w1;
@@ -116,15 +127,15 @@ __device__ __forceinline__ void turn_row(const Turn& r, bool normed, const r_u32
                 float& lo = i < 2 ? a[2 * i] : b[2 * i - 4];
                 float& hi = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
                 const float x = lo, y = hi;
-                lo = x * r.c[i] - y * r.s[i];
-                hi = y * r.c[i] + x * r.s[i];
+                lo = __builtin_fmaf(x, r.c[i], -(y * r.s[i]));
+                hi = __builtin_fmaf(y, r.c[i], x * r.s[i]);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float x = a[i], y = b[i];
-                a[i] = x * r.c[i] - y * r.s[i];
-                b[i] = y * r.c[i] + x * r.s[i];
+                a[i] = __builtin_fmaf(x, r.c[i], -(y * r.s[i]));
+                b[i] = __builtin_fmaf(y, r.c[i], x * r.s[i]);
             }
         }
     }
@@ -132,160 +143,222 @@ __device__ __forceinline__ void turn_row(const Turn& r, bool normed, const r_u32
     x1 = r_u32x2{ E::pack(b[0], b[1]), E::pack(b[2], b[3]) };
 }
 
-// Heads h0 + first, h0 + first + step, .. below h1 of one token: `src` its row of head 0, `put(head, piece 0, piece 1)` takes them away.
-template <int D, class E, class Put>
-__device__ __forceinline__ void turn_heads(const Turn& r, const uint16_t* __restrict__ src, const uint16_t* __restrict__ norm, float eps,
-                                           int32_t first, int32_t end, int32_t step, bool there, Put put)
-{
-    r_u32x2 w[2] = {{0u, 0u}, {0u, 0u}};
-    if (norm) {
-        w[0] = *(const r_u32x2*)(norm + r.off0);
-        w[1] = *(const r_u32x2*)(norm + r.off1);
+// A thread's part of a norm's weights.
+struct Weights {
+    r_u32x2 w[2];
+    bool there;
+    __device__ __forceinline__ Weights(const Turn& r, const uint16_t* __restrict__ norm) : there(norm != nullptr) {
+        w[0] = w[1] = r_u32x2{0u, 0u};
+        if (norm) {
+            w[0] = *(const r_u32x2*)(norm + r.off0);
+            w[1] = *(const r_u32x2*)(norm + r.off1);
+        }
     }
-    for (int32_t h = first; h < end; h += kRopeRows * step) {
-        r_u32x2 x[kRopeRows][2];
+};
+
+// kRopeRows rows of a thread, heads h, h + step, .. below end.
+template <int D>
+struct Rows {
+    r_u32x2 x[kRopeRows][2];
+    __device__ __forceinline__ Rows(const Turn& r, const uint16_t* __restrict__ src, int32_t h, int32_t step, int32_t end, bool there) {
 #pragma unroll
         for (int i = 0; i < kRopeRows; ++i) {
-            const int32_t head = min(h + i * step, end - 1);
             x[i][0] = x[i][1] = r_u32x2{0u, 0u};
-            if (there) {
-                x[i][0] = *(const r_u32x2*)(src + head * D + r.off0);
-                x[i][1] = *(const r_u32x2*)(src + head * D + r.off1);
+            if (there && h + i * step < end) {
+                x[i][0] = *(const r_u32x2*)(src + (h + i * step) * D + r.off0);
+                x[i][1] = *(const r_u32x2*)(src + (h + i * step) * D + r.off1);
             }
         }
+    }
+    template <class E, class Put>
+    __device__ __forceinline__ void finish(const Turn& r, const Weights& w, float eps, int32_t h, int32_t step, int32_t end, bool there, Put put) {
 #pragma unroll
         for (int i = 0; i < kRopeRows; ++i) {
-            if (h + i * step >= end) break;
-            turn_row<D, E>(r, norm != nullptr, w, eps, x[i][0], x[i][1]);
-            if (there) put(h + i * step, x[i][0], x[i][1]);
+            turn_row<D, E>(r, w.there, w.w, eps, x[i][0], x[i][1]);
+            if (there && h + i * step < end) put(h + i * step, x[i][0], x[i][1]);
         }
+    }
+};
+
+// The sequence of token t.  In an online-first batch it is usually sequence t: that is tried before bisecting the prefix sums.
+__device__ __forceinline__ int32_t sequence_of(const RopeArgs& a, int32_t t) {
+    const int32_t s = min(t, a.S - 1);
+    if (a.cu_q_lens[s] <= t && t < a.cu_q_lens[s + 1]) return s;
+    int32_t lo = 0, hi = a.S;                                    // cu[lo] <= t < cu[hi]
+    while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) >> 1;
+        if (a.cu_q_lens[mid] <= t) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// One wavefront: heads of one token, from rows to rows; with a cache, K and V of a sequence's single token to its page.
+template <int D, class E, bool kAppend>
+__device__ __forceinline__ void rope_unit(const RopeArgs& a, int32_t unit)
+{
+    constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes, kUnitHeads = kRopeRows * kAtOnce;
+    const bool is_q = unit < a.T * a.q_units;
+    const int32_t at = is_q ? unit : unit - a.T * a.q_units, each = is_q ? a.q_units : a.kv_units;
+    const int32_t t = at / each, c = at - t * each;
+    if (t >= (is_q ? a.T : a.kv_tokens)) return;
+    const int32_t lane = threadIdx.x & 63, j = lane % kLanes;
+    Turn r;
+    turn_places(r, a, j);
+    const int32_t H = is_q ? a.Hq : a.Hkv, h = c * kUnitHeads + lane / kLanes;
+    Rows<D> rows(r, is_q ? a.q + t * a.q_stride : a.k + t * a.k_stride, h, kAtOnce, H, true);
+    const Weights w(r, is_q ? a.q_norm : a.k_norm);
+    int32_t position = 0, seq = 0;
+    if (kAppend && (!a.positions || !is_q)) {
+        seq = sequence_of(a, t);
+        const int32_t first = a.cu_q_lens[seq];
+        position = a.ctx_lens[seq] + (t - first);
+        if (!is_q && a.cu_q_lens[seq + 1] - first != 1) return;  // more tokens than one: the workgroups that fill pages
+    }
+    if (is_q || !kAppend) {
+        turn_angles(r, a, j, t, position);
+        uint16_t* dst = (is_q ? a.q_out : a.k_out) + (int64_t)t * H * D;
+        rows.template finish<E>(r, w, a.eps, h, kAtOnce, H, true, [&](int32_t head, r_u32x2 x0, r_u32x2 x1) {
+            __builtin_nontemporal_store(x0, (r_u32x2*)(dst + head * D + r.off0));
+            __builtin_nontemporal_store(x1, (r_u32x2*)(dst + head * D + r.off1));
+        });
+        return;
+    }
+    r_u32x4 v[kRopeRows];
+#pragma unroll
+    for (int i = 0; i < kRopeRows; ++i) {
+        v[i] = r_u32x4{0u, 0u, 0u, 0u};
+        if (h + i * kAtOnce < H) v[i] = *(const r_u32x4*)(a.v + t * a.v_stride + (h + i * kAtOnce) * D + 8 * j);
+    }
+    const int32_t entry = position / a.page_size, slot = position - entry * a.page_size;
+    const int32_t id = entry < a.max_blocks ? a.block_tables[(int64_t)seq * a.max_blocks + entry] : -1;
+    turn_angles(r, a, j, t, position);
+    if (id < 0 || id >= a.num_pages) return;
+    uint16_t* page = a.layer_base + (int64_t)id * a.page_stride;
+    const int32_t block_elems = a.page_size * D;
+    rows.template finish<E>(r, w, a.eps, h, kAtOnce, H, true, [&](int32_t head, r_u32x2 x0, r_u32x2 x1) {
+        // unit f / 8 of token `slot`, the half of it that the piece is
+        uint16_t* blk = page + (int64_t)head * block_elems + slot * 8;
+        *(r_u32x2*)(blk + (r.off0 >> 3) * a.page_size * 8 + (r.off0 & 7)) = x0;
+        *(r_u32x2*)(blk + (r.off1 >> 3) * a.page_size * 8 + (r.off1 & 7)) = x1;
+    });
+    // V as it is.  feature d of token t: (((d/16) * groups of 8 + t/8) * 16 + d%16) * 8 + t%8
+#pragma unroll
+    for (int i = 0; i < kRopeRows; ++i) {
+        const int32_t head = h + i * kAtOnce;
+        if (head >= H) break;
+        uint16_t* dst = page + (int64_t)(a.Hkv + head) * block_elems + (((j >> 1) * (a.page_size >> 3) + (slot >> 3)) * 16 + (j & 1) * 8) * 8 + (slot & 7);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dst[e * 8] = (uint16_t)(v[i][e >> 1] >> (e & 1) * 16);
     }
 }
 
-// A workgroup: 16 tokens (of one page's positions, or packed ones), the heads of one of a.groups parts.
-template <int D, class E, bool kAppend>
-__global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a)
+// K and V of the 16 positions of a slot, heads kv0 .. of one part; kRopeRows * kHeads heads a round.
+template <int D, class E>
+__device__ __forceinline__ void rope_slot(const RopeArgs& a, int32_t block)
 {
     constexpr int kLanes = D / 8;                                // threads of a row
     constexpr int kHeads = kRopeThreads / (kLanes * kRopeTokens);// heads at once
-    __shared__ uint16_t v_tile[2][kHeads][kRopeTokens][D + 8];
+    __shared__ uint16_t k_tile[kRopeRows][kHeads][kRopeTokens][D + 8], v_tile[kRopeRows][kHeads][kRopeTokens][D + 8];
     const int32_t tid = threadIdx.x, j = tid % kLanes, tok = tid / kLanes % kRopeTokens, sub = tid / (kLanes * kRopeTokens);
-    const int32_t kv0 = (int32_t)((int64_t)blockIdx.y * a.Hkv / a.groups), kv1 = (int32_t)((int64_t)(blockIdx.y + 1) * a.Hkv / a.groups);
-    const int32_t G = a.Hq / a.Hkv;
-    int32_t t = -1, position = 0, entry = -1, slot = 0, seq = 0;
-    const bool slots = kAppend && (int32_t)blockIdx.x < a.slot_blocks;
-    int32_t p0 = 0, first = 0, last = 0;                         // slots: first of the 16 positions; the step fills [first, last)
-    if (slots) {
-        // start(s) = cu_q_lens[s] / 16 + 2 s, as in the append without rotation
-        const OwnedBy own = owner_of(a.cu_q_lens, a.ctx_lens, 0, a.S, (int32_t)blockIdx.x, [](int32_t c, int32_t i) { return (c >> 4) + 2 * i; });
-        first = own.ctx;
-        last = first + own.q_len;
-        if (own.q_len <= 1) return;                              // single tokens: the workgroups behind these
-        p0 = ((first >> 4) + ((int32_t)blockIdx.x - ((own.token >> 4) + 2 * own.seq))) << 4;
-        if (p0 >= last) return;
-        seq = own.seq;
-        position = p0 + tok;
-        if (position >= first && position < last) t = own.token + (position - first);
-    } else {
-        t = ((int32_t)blockIdx.x - (kAppend ? a.slot_blocks : 0)) * kRopeTokens + tok;
-        if (t >= a.T) t = -1;
-        if (kAppend && t >= 0) {
-            // in an online-first batch token t is usually sequence t
-            seq = min(t, a.S - 1);
-            if (!(a.cu_q_lens[seq] <= t && t < a.cu_q_lens[seq + 1])) {
-                int32_t lo = 0, hi = a.S;                        // cu[lo] <= t < cu[hi]
-                while (hi - lo > 1) {
-                    const int32_t mid = (lo + hi) >> 1;
-                    if (a.cu_q_lens[mid] <= t) lo = mid; else hi = mid;
-                }
-                seq = lo;
-            }
-            position = a.ctx_lens[seq];
-            if (a.cu_q_lens[seq + 1] - a.cu_q_lens[seq] != 1) t = -1;
-        }
-    }
-    const bool there = t >= 0;
-    uint16_t* page = nullptr;                                    // the token's page of this layer
-    if (kAppend && there) {
-        entry = position / a.page_size;
-        slot = position - entry * a.page_size;
-        const int32_t id = entry < a.max_blocks ? a.block_tables[(int64_t)seq * a.max_blocks + entry] : -1;
-        if (id >= 0 && id < a.num_pages) page = a.layer_base + (int64_t)id * a.page_stride;
-    }
-    const Turn r = turn_of<D>(a, j, there ? t : 0, position);
-    const int64_t row = there ? t : 0;
-    turn_heads<D, E>(r, a.q + row * a.q_stride, a.q_norm, a.eps, kv0 * G + sub, kv1 * G, kHeads, there,
-                     [&](int32_t h, r_u32x2 x0, r_u32x2 x1) {
-        uint16_t* dst = a.q_out + (row * a.Hq + h) * D;
-        *(r_u32x2*)(dst + r.off0) = x0;
-        *(r_u32x2*)(dst + r.off1) = x1;
-    });
-    const int32_t block_elems = a.page_size * D;
-    turn_heads<D, E>(r, a.k + row * a.k_stride, a.k_norm, a.eps, kv0 + sub, kv1, kHeads, there && (!kAppend || page),
-                     [&](int32_t h, r_u32x2 x0, r_u32x2 x1) {
-        if constexpr (kAppend) {
-            // unit f / 8 of token `slot`, the half of it that the piece is
-            uint16_t* blk = page + (int64_t)h * block_elems + slot * 8;
-            *(r_u32x2*)(blk + (r.off0 >> 3) * a.page_size * 8 + (r.off0 & 7)) = x0;
-            *(r_u32x2*)(blk + (r.off1 >> 3) * a.page_size * 8 + (r.off1 & 7)) = x1;
-        } else {
-            uint16_t* dst = a.k_out + (row * a.Hkv + h) * D;
-            *(r_u32x2*)(dst + r.off0) = x0;
-            *(r_u32x2*)(dst + r.off1) = x1;
-        }
-    });
-    if constexpr (kAppend) {
-        // V as it is.  feature d of token t: (((d/16) * groups of 8 + t/8) * 16 + d%16) * 8 + t%8
-        const int32_t vgroups = a.page_size >> 3;
-        const uint16_t* vrow = a.v + row * a.v_stride + 8 * j;
-        if (!slots) {
-            for (int32_t h = kv0 + sub; h < kv1; h += kHeads) {
-                if (!page) break;
-                const r_u32x4 x = *(const r_u32x4*)(vrow + h * D);
-                uint16_t* dst = page + (int64_t)(a.Hkv + h) * block_elems + (((j >> 1) * vgroups + (slot >> 3)) * 16 + (j & 1) * 8) * 8 + (slot & 7);
+    const int32_t slot_id = block / a.slot_groups, part = block - slot_id * a.slot_groups;
+    const int32_t kv0 = (int32_t)((int64_t)part * a.Hkv / a.slot_groups), kv1 = (int32_t)((int64_t)(part + 1) * a.Hkv / a.slot_groups);
+    // start(s) = cu_q_lens[s] / 16 + 2 s, as in the append without rotation
+    const OwnedBy own = owner_of(a.cu_q_lens, a.ctx_lens, 0, a.S, slot_id, [](int32_t c, int32_t i) { return (c >> 4) + 2 * i; });
+    if (own.q_len <= 1) return;                                  // single tokens: rope_unit
+    const int32_t first = own.ctx, last = first + own.q_len;     // the step fills positions [first, last)
+    const int32_t p0 = ((first >> 4) + (slot_id - ((own.token >> 4) + 2 * own.seq))) << 4;
+    if (p0 >= last) return;
+    const int32_t position = p0 + tok, t = own.token + (position - first);
+    const bool there = position >= first && position < last;
+    Turn r;
+    turn_places(r, a, j);
+    const int64_t row = there ? t : own.token;
+    const uint16_t *k_row = a.k + row * a.k_stride, *v_row = a.v + row * a.v_stride + 8 * j;
+    const int32_t* table = a.block_tables + (int64_t)own.seq * a.max_blocks;
+    auto page_of = [&](int32_t pos) -> uint16_t* {
+        const int32_t entry = pos / a.page_size, id = entry < a.max_blocks ? table[entry] : -1;
+        return id >= 0 && id < a.num_pages ? a.layer_base + (int64_t)id * a.page_stride : nullptr;
+    };
+    // a thread's part of the way out: of K the unit of features 8 fb .. + 7 of a token, of V that of one feature of the 8 positions of a half
+    const int32_t k_tok = tid % kRopeTokens, fb = tid / kRopeTokens % kLanes, k_pos = p0 + k_tok;
+    const int32_t f = tid % D, half = tid / D % 2, vpos = p0 + 8 * half, vgroups = a.page_size >> 3, block_elems = a.page_size * D;
+    uint16_t *k_page = nullptr, *v_page = nullptr;
+    const Weights w(r, a.k_norm);
+    for (int32_t hb = kv0; hb < kv1; hb += kRopeRows * kHeads) {
+        const int32_t h = hb + sub;
+        Rows<D> k(r, k_row, h, kHeads, kv1, there);
+        r_u32x4 v[kRopeRows];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dst[e * 8] = (uint16_t)(x[e >> 1] >> (e & 1) * 16);
-            }
-            return;
+        for (int i = 0; i < kRopeRows; ++i) {
+            v[i] = r_u32x4{0u, 0u, 0u, 0u};
+            if (there && h + i * kHeads < kv1) v[i] = *(const r_u32x4*)(v_row + (h + i * kHeads) * D);
         }
-        // 16 rows become the page's units (one feature of 8 tokens each) through LDS, so that stores are 16 bytes wide
-        const int32_t f = tid % D, half = tid / D % 2, vpos = p0 + 8 * half;
-        const int32_t id_entry = vpos / a.page_size;
-        const int32_t id = id_entry < a.max_blocks && vpos < last ? a.block_tables[(int64_t)seq * a.max_blocks + id_entry] : -1;
-        const bool full = vpos >= first && vpos + 8 <= last;
-        for (int32_t h = kv0, n = 0; h < kv1; h += kHeads, n ^= 1) {
-            if (there && h + sub < kv1) *(r_u32x4*)&v_tile[n][sub][tok][8 * j] = *(const r_u32x4*)(vrow + (h + sub) * D);
-            __syncthreads();
-            if (id < 0 || id >= a.num_pages || h + sub >= kv1) continue;
-            uint16_t* dst = a.layer_base + (int64_t)id * a.page_stride + (int64_t)(a.Hkv + h + sub) * block_elems +
-                            (((f >> 4) * vgroups + (a.page_size == 16 ? half : 0)) * 16 + (f & 15)) * 8;
+        if (hb == kv0) {
+            if (k_pos >= first && k_pos < last) k_page = page_of(k_pos);
+            if (vpos < last && vpos + 8 > first) v_page = page_of(vpos);
+            turn_angles(r, a, j, (int32_t)row, position);
+        } else {
+            __syncthreads();                                     // everybody has read the tiles before
+        }
+#pragma unroll
+        for (int i = 0; i < kRopeRows; ++i) *(r_u32x4*)&v_tile[i][sub][tok][8 * j] = v[i];
+        k.template finish<E>(r, w, a.eps, h, kHeads, kv1, there, [&](int32_t head, r_u32x2 x0, r_u32x2 x1) {
+            uint16_t* to = k_tile[(head - h) / kHeads][sub][tok];
+            *(r_u32x2*)(to + r.off0) = x0;
+            *(r_u32x2*)(to + r.off1) = x1;
+        });
+        // 16 rows become the page's units through LDS, so that stores are 16 bytes wide and a wavefront's lie side by side
+        __syncthreads();
+        if (k_page) {
+#pragma unroll
+            for (int i = 0; i < kRopeRows; ++i)
+                if (h + i * kHeads < kv1)
+                    *(r_u32x4*)(k_page + (int64_t)(h + i * kHeads) * block_elems + (fb * a.page_size + (k_pos & (a.page_size - 1))) * 8) = *(const r_u32x4*)&k_tile[i][sub][k_tok][8 * fb];
+        }
+        if (!v_page) continue;
+#pragma unroll
+        for (int i = 0; i < kRopeRows; ++i) {
+            if (h + i * kHeads >= kv1) break;
+            uint16_t* dst = v_page + (int64_t)(a.Hkv + h + i * kHeads) * block_elems + (((f >> 4) * vgroups + (a.page_size == 16 ? half : 0)) * 16 + (f & 15)) * 8;
             uint16_t e[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = v_tile[n][sub][8 * half + i][f];
-            if (full) {
+            for (int n = 0; n < 8; ++n) e[n] = v_tile[i][sub][8 * half + n][f];
+            if (vpos >= first && vpos + 8 <= last) {
                 *(r_u32x4*)dst = r_u32x4{ (uint32_t)e[0] | (uint32_t)e[1] << 16, (uint32_t)e[2] | (uint32_t)e[3] << 16,
                                           (uint32_t)e[4] | (uint32_t)e[5] << 16, (uint32_t)e[6] | (uint32_t)e[7] << 16 };
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (vpos + i >= first && vpos + i < last) dst[i] = e[i];
+                for (int n = 0; n < 8; ++n)
+                    if (vpos + n >= first && vpos + n < last) dst[n] = e[n];
             }
         }
     }
 }
 
-// The parts that the heads are dealt in: enough workgroups for four a CU where there are heads enough.
-static int32_t head_groups(int64_t blocks, int32_t Hkv) {
-    const int64_t want = (4ll * device_cus() + blocks - 1) / std::max<int64_t>(blocks, 1);
-    return (int32_t)std::min<int64_t>(std::max<int64_t>(want, 1), Hkv);
+// The workgroups that fill pages first (with their chain of trips), then those of rows.
+template <int D, class E, bool kAppend>
+__global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a)
+{
+    if constexpr (kAppend) {
+        const int32_t slots = a.slot_blocks * a.slot_groups;
+        if ((int32_t)blockIdx.x < slots) rope_slot<D, E>(a, (int32_t)blockIdx.x);
+        else rope_unit<D, E, true>(a, ((int32_t)blockIdx.x - slots) * (kRopeThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    } else {
+        rope_unit<D, E, false>(a, (int32_t)blockIdx.x * (kRopeThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    }
 }
 
+// kv_tokens: wavefronts for K too, of the tokens in front of this one (all of them without a cache; the last single one with it).
 template <bool kAppend>
-static int launch_rope(const RopeArgs& args, int32_t D, int64_t blocks, bool f16, hipStream_t st) {
+static int launch_rope(const RopeArgs& args, int32_t D, int32_t kv_tokens, bool f16, hipStream_t st) {
     RopeArgs a = args;
-    if (blocks > 2147483647ll / kRopeThreads) return CS_ERR_UNSUPPORTED;      // (a launch holds fewer than 2^31 threads along x)
-    a.groups = std::min(head_groups(blocks, a.Hkv), 65535);
-    const dim3 grid((uint32_t)blocks, (uint32_t)a.groups);
+    const int32_t heads = kRopeRows * (512 / D);                 // of a wavefront
+    a.q_units = (a.Hq + heads - 1) / heads;
+    a.kv_units = (a.Hkv + heads - 1) / heads;
+    a.kv_tokens = kv_tokens;
+    const int64_t units = (int64_t)a.T * a.q_units + (int64_t)kv_tokens * a.kv_units, slots = (int64_t)a.slot_blocks * a.slot_groups, blocks = slots + (units + 3) / 4;
+    if (units > 2147483647ll - 4 || blocks > 2147483647ll / kRopeThreads) return CS_ERR_UNSUPPORTED;     // (a launch holds fewer than 2^31 threads along x)
+    const dim3 grid((uint32_t)blocks);
     if (D == 128) {
         if (f16) hipLaunchKernelGGL((rope_kernel<128, F16, kAppend>), grid, dim3(kRopeThreads), 0, st, a);
         else     hipLaunchKernelGGL((rope_kernel<128, Bf16, kAppend>), grid, dim3(kRopeThreads), 0, st, a);
@@ -350,7 +423,7 @@ static int qk_rope(const cs_rope* rope, int32_t T, int32_t Hq, int32_t Hkv, int3
     if (rc) return rc;
     if (!k_out || !aligned(k_out, 16)) return CS_ERR_INVALID_ARG;
     a.k_out = (uint16_t*)k_out;
-    return launch_rope<false>(a, D, ((int64_t)T + kRopeTokens - 1) / kRopeTokens, f16, (hipStream_t)stream);
+    return launch_rope<false>(a, D, T, f16, (hipStream_t)stream);
 }
 
 static int append_rope(const cs_kv_pool* pool, int32_t layer, const cs_batch* batch, const cs_rope* rope, int32_t Hq, const void* q, int64_t q_stride,
@@ -371,14 +444,16 @@ static int append_rope(const cs_kv_pool* pool, int32_t layer, const cs_batch* ba
     a.page_stride = pool->page_stride; a.num_pages = pool->num_pages; a.page_size = pool->page_size;
     a.S = batch->num_seqs; a.max_blocks = batch->max_blocks_per_seq;
     a.block_tables = batch->block_tables; a.ctx_lens = batch->ctx_lens; a.cu_q_lens = batch->cu_q_lens;
-    bool any_single = false, any_chunk = false;
+    int32_t single_end = 0;
+    bool any_chunk = false;
     for (int32_t s = 0; s < a.S; ++s) {
         const int32_t n = batch->h_cu_q_lens[s + 1] - batch->h_cu_q_lens[s];
-        any_single |= n == 1;
+        if (n == 1) single_end = batch->h_cu_q_lens[s + 1];
         any_chunk |= n > 1;
     }
     a.slot_blocks = any_chunk ? a.T / 16 + 2 * a.S : 0;
-    return launch_rope<true>(a, D, (int64_t)a.slot_blocks + (any_single ? ((int64_t)a.T + kRopeTokens - 1) / kRopeTokens : 0), f16, (hipStream_t)stream);
+    a.slot_groups = (Hkv + 256 / D - 1) / (256 / D);             // a round of heads each
+    return launch_rope<true>(a, D, single_end, f16, (hipStream_t)stream);
 }
 
 }  // namespace cs
