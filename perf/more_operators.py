@@ -315,7 +315,7 @@ def _prepare_verify(case, seed):
          "count": torch.empty(len(trees), dtype=torch.int32, device="cuda")}
     if own:
         from paper_2410_01228_amd import binding as cs
-        s["batch"] = cs.Batch(torch.zeros((len(trees), 1), dtype=torch.int32), torch.zeros(len(trees), dtype=torch.int32), cu)
+        s["batch"] = cs.Batch(torch.zeros((len(trees), _blocks(max(len(t) for t in trees))), dtype=torch.int32), torch.zeros(len(trees), dtype=torch.int32), cu)
         s["workspace"] = cs.workspace_for_verify(s["batch"], vocab)
     return s
 
