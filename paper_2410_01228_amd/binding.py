@@ -187,18 +187,18 @@ def lib():
         L.cs_kv_pages_free.restype, L.cs_kv_pages_free.argtypes = ctypes.c_int, [TP, vp, i32, vp, vp, vp]
         L.cs_kv_pages_compact_workspace_bytes.restype, L.cs_kv_pages_compact_workspace_bytes.argtypes = sz, [i32]
         L.cs_kv_pages_compact.restype, L.cs_kv_pages_compact.argtypes = ctypes.c_int, [SP, i32, i32, TP, TP, vp, vp, vp, sz, vp]
-        RP, i64 = ctypes.POINTER(cs_rope), ctypes.c_int64
+        i64 = ctypes.c_int64                            # (structs of the calls below go as bare addresses: converting typed pointers costs the host 0.1 us each)
         for f in (L.cs_qk_rope, L.cs_qk_rope_f16):
-            f.restype, f.argtypes = ctypes.c_int, [RP, i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp]
+            f.restype, f.argtypes = ctypes.c_int, [vp, i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp]
         for f in (L.cs_kv_append_rope, L.cs_kv_append_rope_f16):
-            f.restype, f.argtypes = ctypes.c_int, [PP, i32, BP, RP, i32, vp, i64, vp, i64, vp, i64, vp, vp]
+            f.restype, f.argtypes = ctypes.c_int, [vp, i32, vp, vp, i32, vp, i64, vp, i64, vp, i64, vp, vp]
         L.cs_paged_attention_tree_workspace_bytes.restype = sz
         L.cs_paged_attention_tree_workspace_bytes.argtypes = [BP, i32, i32, i32]
         for f in (L.cs_paged_attention_tree, L.cs_paged_attention_tree_f16):
-            f.restype, f.argtypes = ctypes.c_int, [PP, i32, BP, vp, vp, i32, ctypes.c_float, vp, i32, vp, sz, vp]
+            f.restype, f.argtypes = ctypes.c_int, [vp, i32, vp, vp, vp, i32, ctypes.c_float, vp, i32, vp, sz, vp]
         L.cs_spec_verify_workspace_bytes.restype, L.cs_spec_verify_workspace_bytes.argtypes = sz, [i32, i32]
-        L.cs_spec_verify.restype, L.cs_spec_verify.argtypes = ctypes.c_int, [BP, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
-        L.cs_kv_tree_commit.restype, L.cs_kv_tree_commit.argtypes = ctypes.c_int, [PP, i32, i32, BP, vp, vp, vp]
+        L.cs_spec_verify.restype, L.cs_spec_verify.argtypes = ctypes.c_int, [vp, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.cs_kv_tree_commit.restype, L.cs_kv_tree_commit.argtypes = ctypes.c_int, [vp, i32, i32, vp, vp, vp, vp]
         L.cs_debug_set_cu_count.restype, L.cs_debug_set_cu_count.argtypes = None, [i32]
         L.cs_debug_copy.restype, L.cs_debug_copy.argtypes = ctypes.c_int, [vp, vp, sz, vp]
         L.cs_set_decode_split_tokens.restype, L.cs_set_decode_split_tokens.argtypes = None, [i32]
@@ -268,6 +268,7 @@ class Pool:
         ps = self.page_elems if page_stride is None else page_stride
         ls = P * ps if layer_stride is None else layer_stride
         self.c = cs_kv_pool(_ptr(tensor), L, P, page_size, Hkv, D, ls, ps)
+        self.at = ctypes.addressof(self.c)
         self.L, self.P, self.Hkv, self.D = L, P, Hkv, D
 
     @classmethod
@@ -344,6 +345,7 @@ class Batch:
         self.max_blocks = int(self.h_bt.shape[1]) if self.h_bt.dim() == 2 and self.h_bt.numel() else 1
         self.c = cs_batch(S, int(self.h_cu[S]), _ptr(self.d_bt), self.max_blocks, _ptr(self.d_ctx),
                           _ptr(self.d_cu), _ptr(self.h_ctx), _ptr(self.h_cu))
+        self.at = ctypes.addressof(self.c)
 
     def truncated(self, num_seqs: int) -> "Batch":
         """The same arrays with only the first num_seqs sequences (what a layer-wise
@@ -352,6 +354,7 @@ class Batch:
         b.__dict__.update(self.__dict__)
         b.c = cs_batch(num_seqs, int(self.h_cu[num_seqs]), _ptr(self.d_bt), self.max_blocks,
                        _ptr(self.d_ctx), _ptr(self.d_cu), _ptr(self.h_ctx), _ptr(self.h_cu))
+        b.at = ctypes.addressof(b.c)
         return b
 
     @property
@@ -688,7 +691,7 @@ class Rope:
         pairs = (ctypes.c_int32 * 3)(*([int(n) for n in axis_pairs] + [0] * (3 - axes) if axes > 1 else (rotary_dim // 2, 0, 0)))
         self.c = cs_rope(_ptr(inv_freq), rotary_dim, int(bool(interleaved)), _ptr(positions), 0 if positions is None or axes == 1 else positions.stride(0), axes, pairs,
                          _ptr(q_norm), _ptr(k_norm), eps)
-        self.ref = ctypes.byref(self.c)
+        self.at = ctypes.addressof(self.c)
 
 
 _16_BITS = (torch.bfloat16, torch.float16)
@@ -708,7 +711,7 @@ def _qk_rope(fn, where, rope: Rope, q, k, q_out, k_out, stream):
     assert rope.most_tokens >= T and rope.most_features >= D
     qp, qs = _head_rows(q, T, Hq, D)
     kp, ks = _head_rows(k, T, Hkv, D)
-    rc = fn(rope.ref, T, Hq, Hkv, D, qp, qs, kp, ks, _rows(q_out, T * Hq * D), _rows(k_out, T * Hkv * D), _stream(stream))
+    rc = fn(rope.at, T, Hq, Hkv, D, qp, qs, kp, ks, _rows(q_out, T * Hq * D), _rows(k_out, T * Hkv * D), _stream(stream))
     if rc:
         raise CsError(rc, where)
 
@@ -728,7 +731,7 @@ def _append_rope(fn, where, pool: Pool, layer, batch: Batch, rope: Rope, q, k_ne
     qp, qs = _head_rows(q, T, Hq, D)
     kp, ks = _head_rows(k_new, T, Hkv, D)
     vp, vs = _head_rows(v_new, T, Hkv, D)
-    rc = fn(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), rope.ref, Hq, qp, qs, kp, ks, vp, vs, _rows(q_out, T * Hq * D), _stream(stream))
+    rc = fn(pool.at, layer, batch.at, rope.at, Hq, qp, qs, kp, ks, vp, vs, _rows(q_out, T * Hq * D), _stream(stream))
     if rc:
         raise CsError(rc, where)
 
@@ -760,7 +763,7 @@ def _tree(fn, where, pool: Pool, layer, batch: Batch, q, out, Hq, softmax_scale,
         assert rows >= T and tree_mask.element_size() == 8 and tree_mask.is_contiguous()
         mask = tree_mask.data_ptr()
     ws, wb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    rc = fn(ctypes.byref(pool.c), layer, ctypes.byref(batch.c), _rows(q, n), _rows(out, n), Hq, softmax_scale, mask, words, ws, wb, _stream(stream))
+    rc = fn(pool.at, layer, batch.at, _rows(q, n), _rows(out, n), Hq, softmax_scale, mask, words, ws, wb, _stream(stream))
     if rc:
         raise CsError(rc, where)
 
@@ -803,14 +806,14 @@ def cs_spec_verify(batch: Batch, tokens: torch.Tensor, parents: Optional[torch.T
     pp, ps = _prob_rows(p, T, vocab)
     qp, qs = (None, 0) if q is None else _prob_rows(q, T, vocab)
     ws, wb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    rc = lib().cs_spec_verify(ctypes.byref(batch.c), vocab, _list(tokens, T), None if parents is None else _list(parents, T), pp, ps, qp, qs, _floats(u, T), _floats(u_next, S),
+    rc = lib().cs_spec_verify(batch.at, vocab, _list(tokens, T), None if parents is None else _list(parents, T), pp, ps, qp, qs, _floats(u, T), _floats(u_next, S),
                               _list(out_tokens, T), _list(path, T), _list(count, S), ws, wb, _stream(stream))
     if rc:
         raise CsError(rc, "cs_spec_verify")
 
 
 def cs_kv_tree_commit(pool: Pool, layer_begin: int, layer_end: int, batch: Batch, path: torch.Tensor, count: torch.Tensor, stream=None):
-    rc = lib().cs_kv_tree_commit(ctypes.byref(pool.c), layer_begin, layer_end, ctypes.byref(batch.c), _list(path, batch.c.num_tokens), _list(count, batch.c.num_seqs),
+    rc = lib().cs_kv_tree_commit(pool.at, layer_begin, layer_end, batch.at, _list(path, batch.c.num_tokens), _list(count, batch.c.num_seqs),
                                  _stream(stream))
     if rc:
         raise CsError(rc, "cs_kv_tree_commit")

@@ -24,7 +24,7 @@ namespace cs {
 // finishes last has all block sums and goes on alone.  Where it finds that the walk needs a further row (a node with
 // several drawn children, all but the last of which cost a pass), it makes those passes by itself.
 // ------------------------------------------------------------------------------------
-constexpr int kVerifyWaves = 8;
+constexpr int kVerifyWaves = 16;
 constexpr int kVerifyThreads = kVerifyWaves * 64;
 constexpr int kRowBlock = 1024;                                  // elements that a wavefront sums at once
 constexpr int kMaxRowBlocks = CS_MAX_VOCAB / kRowBlock;
@@ -354,13 +354,16 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
     if (a.parts > 1 && wave == 0) Announcements(Shared(a.words + (int64_t)seq * a.parts, (uint32_t)a.parts * 8), 0, 8, (uint32_t)a.parts, a.launch).clear();
 }
 
-// Workgroups of a sequence: at most as many as its row's blocks keep busy, and as fill the chip four times.
+// Workgroups of a sequence: at most as many as its row's blocks keep busy, and together one a compute unit (what a CU holds: every
+// workgroup begins with the walk's trips to memory, so a second round of them costs those again: 128 chains of 6, 128256 probabilities,
+// 48 us with four, 37 with one).  A row of at most kAlone blocks is one workgroup's: it saves the trips by which several join.
+constexpr int32_t kAlone = 2 * kVerifyWaves;
 struct VerifyPlan { int32_t blocks, parts; size_t words, bytes; };
 static VerifyPlan plan_verify(int32_t S, int32_t vocab) {
     VerifyPlan p;
     p.blocks = (vocab + kRowBlock - 1) / kRowBlock;
     const int32_t most = (p.blocks + kVerifyWaves - 1) / kVerifyWaves;
-    p.parts = (int32_t)std::min<int64_t>(most, std::max<int64_t>(1, (4ll * device_cus() + S - 1) / S));
+    p.parts = p.blocks <= kAlone ? 1 : (int32_t)std::min<int64_t>(most, std::max<int64_t>(1, ((int64_t)device_cus() + S - 1) / S));
     p.words = p.parts > 1 ? (size_t)S * p.parts * 8 : 0;
     p.bytes = p.parts > 1 ? p.words + (size_t)S * p.blocks * 8 : 0;
     p.bytes = (p.bytes + 15) & ~(size_t)15;

@@ -1,6 +1,7 @@
 // Attention of drafted trees over the paged cache: the launch plan and the C entries (kernels: cs_tree_impl.h).
 #include <algorithm>
 #include <new>
+#include <string.h>
 #include <vector>
 #include "cs_plan.h"
 #include "cs_tree.h"
@@ -72,6 +73,32 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
     return p;
 }
 
+// The last plans that the thread made (the workspace query and the calls of the next layers ask for the same one: 64 sequences
+// cost the host 8 us to plan), keyed by everything a plan depends on, the lengths value by value.
+struct TreeMemo {
+    int32_t S = -1, Hq = 0, Hkv = 0, D = 0, cus = 0;
+    std::vector<int32_t> ctx, cu;
+    TreePlan plan;
+};
+static const TreePlan& tree_plan_for(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D) {
+    static thread_local TreeMemo memo[4];
+    static thread_local int next = 0;
+    const int32_t S = b->num_seqs, cus = device_cus();
+    for (TreeMemo& m : memo)
+        if (m.S == S && m.Hq == Hq && m.Hkv == Hkv && m.D == D && m.cus == cus && memcmp(m.ctx.data(), b->h_ctx_lens, sizeof(int32_t) * S) == 0 &&
+            memcmp(m.cu.data(), b->h_cu_q_lens, sizeof(int32_t) * (S + 1)) == 0)
+            return m.plan;
+    TreeMemo& m = memo[next];
+    next = (next + 1) % 4;
+    m.S = -1;                                                    // (no plan while this one is made: memory may run out)
+    m.plan = plan_tree(b, Hq, Hkv, D);
+    m.ctx.assign(b->h_ctx_lens, b->h_ctx_lens + S);
+    m.cu.assign(b->h_cu_q_lens, b->h_cu_q_lens + S + 1);
+    m.Hq = Hq; m.Hkv = Hkv; m.D = D; m.cus = cus;
+    m.S = S;
+    return m.plan;
+}
+
 template <int D, class E, int PS>
 static void launch_tree(const TreePlan& p, const cs_kv_pool& pool, const uint16_t* layer_base, const cs_batch& b, int32_t G, const uint64_t* mask, int32_t mask_words,
                         const uint16_t* q, uint16_t* out, float scale_log2e, const TreePartials& part, const TreeItems& items, int32_t n, hipStream_t st) {
@@ -129,7 +156,7 @@ static int attention_tree(const cs_kv_pool* pool, int32_t layer, const cs_batch*
     if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return CS_ERR_INVALID_ARG;   // positive, finite
     if (mask && (((uintptr_t)mask & 7) || mask_words < (most + 63) / 64 || mask_words > kTreeWords)) return CS_ERR_INVALID_ARG;
     try {
-        const TreePlan p = plan_tree(batch, Hq, Hkv, D);
+        const TreePlan& p = tree_plan_for(batch, Hq, Hkv, D);
         if (p.bytes > 0 && (!workspace || ((uintptr_t)workspace & 15))) return CS_ERR_INVALID_ARG;
         if (workspace_bytes < p.bytes) return CS_ERR_WORKSPACE_TOO_SMALL;
         const int32_t G = Hq / Hkv;
@@ -155,7 +182,7 @@ extern "C" {
 size_t cs_paged_attention_tree_workspace_bytes(const cs_batch* batch, int32_t Hq, int32_t Hkv, int32_t D) {
     if (attention_shape_ok(Hq, Hkv, D) != CS_OK) return 0;
     if (validate_batch(nullptr, batch) != CS_OK || batch->num_seqs == 0 || most_new(batch) > CS_MAX_TREE) return 0;
-    try { return plan_tree(batch, Hq, Hkv, D).bytes; } catch (const std::bad_alloc&) { return 0; }
+    try { return tree_plan_for(batch, Hq, Hkv, D).bytes; } catch (const std::bad_alloc&) { return 0; }
 }
 
 int cs_paged_attention_tree(const cs_kv_pool* pool, int32_t layer, const cs_batch* batch, const void* q, void* out, int32_t num_q_heads, float softmax_scale,
