@@ -76,7 +76,7 @@ __device__ __forceinline__ void load_k(TreeKv<D>& r, const uint16_t* __restrict_
     if constexpr (PS == 8) page = (lane & 8) ? id.b : id.a;
     const char* p = (const char*)(layer_base + (int64_t)page * page_stride + (int64_t)g * (PS * D)) + at.k;
 #pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk) r.k[H][kk] = *(const u32x4*)(p + kk * (PS * 64));
+    for (int kk = 0; kk < D / 32; ++kk) r.k[H][kk] = __builtin_nontemporal_load((const u32x4*)(p + kk * (PS * 64)));
 }
 template <int D, int PS, int H>
 __device__ __forceinline__ void load_v(TreeKv<D>& r, const uint16_t* __restrict__ layer_base, int64_t page_stride, StepIds<PS> id, int32_t g, int32_t Hkv, const TreeLane<D, PS>& at, int lane)
@@ -85,7 +85,7 @@ __device__ __forceinline__ void load_v(TreeKv<D>& r, const uint16_t* __restrict_
     if constexpr (PS == 8) page = (lane & 32) ? id.b : id.a;
     const char* p = (const char*)(layer_base + (int64_t)page * page_stride + (int64_t)(Hkv + g) * (PS * D)) + at.v;
 #pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) r.v[H][dt] = *(const u32x2*)(p + dt * (PS * 32));
+    for (int dt = 0; dt < D / 16; ++dt) r.v[H][dt] = __builtin_nontemporal_load((const u32x2*)(p + dt * (PS * 32)));
 }
 
 // The four weights' sum of the lane's two dwords pairs, as they are after rounding (bf16), or before it (fp16: below 2^-14 the matrix unit keeps
@@ -445,9 +445,13 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
 
     // The wavefront's part of a step's copies: K (even wavefronts) or V of 16-key step wave / 2, a page or a pair of pages of 8.  A step
     // behind the sequence's last one reads that one again: its keys are masked.
+    // Page offsets travel in lane registers, lane j's of 16-key step window + j (pages of 8: of its pair), and are read out with v_readlane: a
+    // scalar load and the 64-bit product behind it, in front of every step's copies, held up the step by 600 cycles.
     constexpr int kCopies = Lds::kBlock / 1024;
-    auto copy = [&](int32_t step) {
-        const int32_t to = min(first + 2 * step + (wave >> 1), step_end - 1);
+    int32_t window = 0;                                          // 16-key step of lane 0, counted from the item's first
+    uint32_t off_lo[PS == 16 ? 1 : 2], off_hi[PS == 16 ? 1 : 2];
+    auto load_window = [&] {
+        const int32_t to = min(first + window + lane, step_end - 1);
         StepIds<PS> id;
         if constexpr (PS == 16) {
             id.a = table[to];
@@ -456,17 +460,38 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
             id.b = table[min(2 * to + 1, n_entries - 1)];
         }
         id = loadable<PS>(id, num_pages);
-        char* dst = lds.ring[(uint32_t)step % kTreeRing] + (wave & 1 ? 2 * Lds::kBlock + 64 + (wave >> 1) * Lds::kBlock : (wave >> 1) * (Lds::kBlock + 64));
         const int64_t block = (int64_t)((wave & 1 ? Hkv : 0) + g) * (PS * D);
+        auto put = [&](int k, int32_t page) {
+            const uint64_t off = ((uint64_t)page * (uint64_t)page_stride + (uint64_t)block) * 2;
+            off_lo[k] = (uint32_t)off;
+            off_hi[k] = (uint32_t)(off >> 32);
+        };
+        put(0, id.a);
+        if constexpr (PS == 8) put(1, id.b);
+        // (the load is waited for here, not at every readlane)
+        if constexpr (PS == 16) asm volatile("" : "+v"(off_lo[0]), "+v"(off_hi[0]));
+        else asm volatile("" : "+v"(off_lo[0]), "+v"(off_hi[0]), "+v"(off_lo[1]), "+v"(off_hi[1]));
+    };
+    load_window();
+    auto copy = [&](int32_t step) {
+        if (2 * step - window >= 64) {                           // (steps only ever grow)
+            window += 64;
+            load_window();
+        }
+        const int32_t at = 2 * step - window + (wave >> 1);
+        auto page_at = [&](int k) {
+            const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_hi[k], at) << 32 | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_lo[k], at);
+            return (const char*)layer_base + off;
+        };
+        char* dst = lds.ring[(uint32_t)step % kTreeRing] + (wave & 1 ? 2 * Lds::kBlock + 64 + (wave >> 1) * Lds::kBlock : (wave >> 1) * (Lds::kBlock + 64));
         if constexpr (PS == 16) {
-            const char* src = (const char*)(layer_base + (int64_t)id.a * page_stride + block);
+            const char* src = page_at(0);
 #pragma unroll
             for (int i = 0; i < kCopies; ++i) lds_dma16_one_page(src + i * 1024, (uint32_t)lane * 16, dst + i * 1024);
         } else {
             // K: 8 units a feature block; V: 16 units a feature tile
-            const int32_t page = (wave & 1 ? lane & 16 : lane & 8) ? id.b : id.a;
             const uint32_t off = wave & 1 ? ((lane >> 5) * 16 + (lane & 15)) * 16 : ((lane >> 4) * 8 + (lane & 7)) * 16;
-            const uint64_t src = (uint64_t)(uintptr_t)(layer_base + (int64_t)page * page_stride + block) + off;
+            const uint64_t src = (uint64_t)(uintptr_t)((wave & 1 ? lane & 16 : lane & 8) ? page_at(1) : page_at(0)) + off;
 #pragma unroll
             for (int i = 0; i < kCopies; ++i) lds_dma16_lane_addr<0>(src + i * 512, dst + i * 1024);
         }
@@ -513,6 +538,8 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
         else wait_vmcnt<0>();
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
+    };
+    auto ahead = [&](int32_t i) {
         if (i + kTreeRing - 1 < steps) copy(i + kTreeRing - 1);
     };
     const uint32_t k_at = (lane & 15) / 8 * (Lds::kBlock + 64) + ((lane >> 4) * 16 + ((lane >> 2) & 1) * 8 + (lane & 3)) * 16;
@@ -539,6 +566,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
             u32x4 pb[T > 0 ? T : 1];
 #pragma unroll
             for (int c = 0; c < T; ++c) scores(slot, c, x[c]);
+            ahead(i);                                            // (behind the first reads of this step)
 #pragma unroll
             for (int c = 0; c < T; ++c) pb[c] = tree_weights<D, E, NC, false>(st, c, x[c], scale_log2e);
             if constexpr (T > 0) {
@@ -556,6 +584,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
     if constexpr (NC >= 2) if (tiles == 2) run(std::integral_constant<int, 2>{});
     for (; i < steps; ++i) {
         begin(i);
+        ahead(i);
         const char* slot = lds.ring[(uint32_t)i % kTreeRing];
         const int32_t key0 = key_begin + i * kTreeKeys + (lane >> 4) * 8, valid = n_keys - key0;     // the lane's 8 keys
         u32x4 pb[NC];
