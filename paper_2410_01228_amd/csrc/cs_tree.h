@@ -5,13 +5,22 @@
 namespace cs {
 
 constexpr int kTreeWords = CS_MAX_TREE / 64;                     // mask words of a node at most
-constexpr int kTreeTiles = 8;                                    // column tiles (16 rows) of a workgroup at most
+constexpr int kTreeTiles = 12;                                   // column tiles (16 rows) of a workgroup at most: three a wavefront
 
-// The column tiles of R = nodes * G rows, dealt evenly to as few workgroups as hold them.
+// The column tiles of R = nodes * G rows, dealt evenly to workgroups.  One or two tiles are a workgroup whose wavefronts share the keys.  Otherwise a
+// wavefront has one to three of them, and a workgroup's time goes by its fullest wavefront: the number that leaves the least of
+// four times as many empty is taken, the larger one where they are even (K and V are read once for all of them).
 struct TreeBlocks { int32_t blocks, tiles; };
 __host__ __device__ inline TreeBlocks tree_blocks(int32_t rows) {
-    const int32_t all = (rows + 15) / 16, blocks = (all + kTreeTiles - 1) / kTreeTiles;
-    return {blocks, blocks ? (all + blocks - 1) / blocks : 0};
+    const int32_t all = (rows + 15) / 16;
+    if (all <= 2) return {all > 0 ? 1 : 0, all};
+    int32_t best = 1, least = (all + 3) / 4;
+    for (int32_t each = 2; each <= 3; ++each) {
+        const int32_t cost = (all + 4 * each - 1) / (4 * each) * each;
+        if (cost <= least) { least = cost; best = each; }
+    }
+    const int32_t blocks = (all + 4 * best - 1) / (4 * best);
+    return {blocks, (all + blocks - 1) / blocks};
 }
 
 // Keys of a piece of a sequence of n keys cut into k: whole rounds of the four wavefronts' 32-key steps.

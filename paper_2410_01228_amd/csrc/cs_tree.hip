@@ -1,5 +1,6 @@
 // Attention of drafted trees over the paged cache: the launch plan and the C entries (kernels: cs_tree_impl.h).
 #include <algorithm>
+#include <functional>
 #include <new>
 #include <string.h>
 #include <vector>
@@ -9,9 +10,12 @@
 
 namespace cs {
 
+constexpr int32_t kTreeLeastPiece = 256;                         // keys of a piece, about, at least
+constexpr int32_t kTreeModelled = 2048;                          // workgroups of a kv head up to which launches are modelled
+
 // How a batch is launched: a pure function of the host lengths, the shape and the chip.
 struct TreePlan {
-    int32_t tiles = 0;                                           // column tiles of a workgroup: 1, 2 (wavefronts share the keys), 4 or 8 (they share the rows)
+    int32_t tiles = 0;                                           // column tiles of a workgroup: 1, 2 (wavefronts share the keys), 4, 8 or 12 (they share the rows)
     bool cut = false;                                            // some sequence comes in pieces
     std::vector<uint32_t> items;                                 // in launch order: a sequence's pieces and, innermost, its blocks stand together
     std::vector<int32_t> launches;                               // first items of the launches
@@ -24,15 +28,19 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
     TreePlan p;
     const int32_t G = Hq / Hkv, S = b->num_seqs;
     int32_t most = 1;
-    int64_t whole = 0;
     for (int32_t s = 0; s < S; ++s) {
         const TreeBlocks t = tree_blocks((b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s]) * G);
         most = std::max(most, t.tiles);
-        whole += t.blocks;
     }
-    p.tiles = most <= 1 ? 1 : most <= 2 ? most : most <= 4 ? 4 : 8;
-    // Pieces: of 8192 keys, halved until every CU has two workgroups, or down to 512.
-    const int64_t want = 2ll * device_cus();
+    p.tiles = most <= 1 ? 1 : most <= 2 ? most : (most + 3) / 4 * 4;
+    // Pieces: the length at which a model of the launch ends first.  Workgroups of the chip's slots take the pieces in order, the longest first;
+    // a step costs what it does on a full chip (measured with 512 workgroups of 4064 and 8160 keys, 8 kv heads), and a piece of a cut sequence its partial
+    // result and a share of the merge.  (Halving from 8192 until there were two workgroups a CU, whatever their lengths: FIT.)
+    const int32_t slots = std::max(1, device_cus() * (p.tiles == 2 && D == 128 ? 1 : 2) / Hkv);
+    auto step_us = [&](int32_t tiles) {
+        const double us = tiles <= 2 ? 1.25 : tiles <= 8 ? 1.32 : 1.72;
+        return (D == 64 ? (tiles <= 2 ? 0.5 : 0.6) : p.tiles == 2 ? 0.5 : 1.0) * us;
+    };
     auto pieces_of = [&](int32_t s, int32_t split) {
         const int32_t q = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s], n = b->h_ctx_lens[s] + q, blocks = tree_blocks(q * G).blocks;
         if (blocks == 0) return 0;
@@ -44,11 +52,38 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
         }
         return k;
     };
-    int32_t split = 8192;
-    for (; split > 512; split /= 2) {
-        int64_t n = 0;
-        for (int32_t s = 0; s < S; ++s) n += (int64_t)pieces_of(s, split) * tree_blocks((b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s]) * G).blocks;
-        if (n * Hkv >= want) break;
+    int32_t longest = 1;
+    for (int32_t s = 0; s < S; ++s)
+        if (b->h_cu_q_lens[s + 1] > b->h_cu_q_lens[s]) longest = std::max(longest, b->h_ctx_lens[s] + b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s]);
+    int32_t split = 2 * longest;                                 // (nothing is cut)
+    double least = 0;
+    std::vector<float> work, busy;
+    for (int32_t trial = 2 * longest; ; trial = trial == 2 * longest ? std::max(longest, kTreeLeastPiece) : trial * 4 / 5) {
+        if (trial < kTreeLeastPiece) break;
+        work.clear();
+        double partials = 0;
+        for (int32_t s = 0; s < S; ++s) {
+            const int32_t q = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s], n = b->h_ctx_lens[s] + q, k = pieces_of(s, trial);
+            if (k == 0) continue;
+            const TreeBlocks t = tree_blocks(q * G);
+            const int32_t chunk = tree_chunk_keys(n, k);
+            for (int32_t i = 0; i < k; ++i) {
+                const int32_t keys = std::min(chunk, n - i * chunk);
+                for (int32_t j = 0; j < t.blocks; ++j) work.push_back((float)(8.0 + (keys + 31) / 32 * step_us(t.tiles)));
+            }
+            if (k > 1) partials += (double)k * t.blocks * t.tiles;
+        }
+        if ((int64_t)work.size() > kTreeModelled && trial != 2 * longest) break;    // (pieces enough for an even end)
+        std::sort(work.begin(), work.end(), std::greater<float>());
+        busy.assign(slots, 0.f);                                 // a heap of when the slots come free
+        for (float w : work) {
+            std::pop_heap(busy.begin(), busy.end(), std::greater<float>());
+            busy.back() += w;
+            std::push_heap(busy.begin(), busy.end(), std::greater<float>());
+        }
+        double end = *std::max_element(busy.begin(), busy.end());
+        if (partials > 0) end += 4.0 + partials * Hkv * 16 * D * 8 / 5e6;
+        if (trial == 2 * longest || end < least) { least = end; split = trial; }
     }
     struct Seq { int32_t seq, pieces, blocks, keys; };
     std::vector<Seq> seqs;
@@ -109,7 +144,8 @@ static void launch_tree(const TreePlan& p, const cs_kv_pool& pool, const uint16_
     if (p.tiles == 1) CS_LAUNCH_TREE(tree_kernel, 1);
     else if (p.tiles == 2) CS_LAUNCH_TREE(tree_kernel, 2);
     else if (p.tiles == 4) CS_LAUNCH_TREE(tree_ring_kernel, 1);
-    else CS_LAUNCH_TREE(tree_ring_kernel, 2);
+    else if (p.tiles == 8) CS_LAUNCH_TREE(tree_ring_kernel, 2);
+    else CS_LAUNCH_TREE(tree_ring_kernel, 3);
 #undef CS_LAUNCH_TREE
 }
 

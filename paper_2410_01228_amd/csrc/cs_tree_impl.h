@@ -7,7 +7,7 @@
 //   O^T[d][row]  += V^T . P^T          v_mfma_f32_16x16x32, 32 keys: two steps' keys, four consecutive ones of either a lane group
 // with an online softmax per row in fp32.  K and V come from HBM into the operand registers as in decode (cs_decode_impl.h: the page
 // format is the operand layout), and each page read serves up to kTreeTiles column tiles: a workgroup is
-// (sequence, kv head, key range, block of up to 128 rows), its wavefronts take 32-key steps in turn.  Bound by HBM up to some 128 rows a kv
+// (sequence, kv head, key range, block of up to 192 rows), its wavefronts take 32-key steps in turn.  Bound by HBM up to some 128 rows a kv
 // head and beyond that by the matrix unit and the softmax's vector instructions.
 #pragma once
 #include "cs_decode_impl.h"
@@ -582,6 +582,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
     if (tiles == 0) run(std::integral_constant<int, 0>{});
     if (tiles == 1) run(std::integral_constant<int, 1>{});
     if constexpr (NC >= 2) if (tiles == 2) run(std::integral_constant<int, 2>{});
+    if constexpr (NC >= 3) if (tiles == 3) run(std::integral_constant<int, 3>{});
     for (; i < steps; ++i) {
         begin(i);
         ahead(i);
@@ -664,14 +665,35 @@ __global__ __launch_bounds__(kDecodeThreads) void tree_merge_kernel(
         float M = -INFINITY, L = 0.f;
         f32x4 O = {0.f, 0.f, 0.f, 0.f};
         const int64_t at = ((int64_t)(items.base + item) * Hkv + g) * part_rows + c * 16 + r, next = (int64_t)blocks.blocks * Hkv * part_rows;
-        for (int32_t i = 0; i < it.pieces; ++i) M = fmaxf(M, part.ml[(at + i * next) * 2]);
-        for (int32_t i = 0; i < it.pieces; ++i) {
-            const float m = part.ml[(at + i * next) * 2], l = part.ml[(at + i * next) * 2 + 1];
-            const f32x4 o = *(const f32x4*)(part.o + (at + i * next) * D + d);
-            if (m == -INFINITY && l == 0.f) continue;
-            const float f = exp2f(m - M);
-            L += l * f;
-            O += o * f;
+        // eight pieces' loads in flight at once; with more of them the maxima are read twice
+        for (int32_t i0 = 0; it.pieces > 8 && i0 < it.pieces; i0 += 8) {
+            float m[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m[i] = part.ml[(at + min(i0 + i, it.pieces - 1) * next) * 2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) M = fmaxf(M, m[i]);
+        }
+        for (int32_t i0 = 0; i0 < it.pieces; i0 += 8) {
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            f32x2 ml[8];
+            f32x4 o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {                        // (past the last piece: the last again)
+                const int64_t p = at + min(i0 + i, it.pieces - 1) * next;
+                ml[i] = *(const f32x2*)(part.ml + p * 2);
+                o[i] = *(const f32x4*)(part.o + p * D + d);
+            }
+            if (it.pieces <= 8) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) M = fmaxf(M, ml[i][0]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i0 + i >= it.pieces || (ml[i][0] == -INFINITY && ml[i][1] == 0.f)) continue;     // (not a weight of zero: an infinity in V stays one)
+                const float f = exp2f(ml[i][0] - M);
+                L += ml[i][1] * f;
+                O += o[i] * f;
+            }
         }
         const int32_t node = row / G, head = row - node * G;
         u32x2 w = {0u, 0u};
