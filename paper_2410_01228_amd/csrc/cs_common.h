@@ -29,6 +29,12 @@ int32_t device_cus();
 // Host-side checks common to every entry point.  Return CS_OK or the error.
 int validate_pool(const cs_kv_pool* pool);
 int validate_batch(const cs_kv_pool* pool, const cs_batch* batch);
+// Whether positions, rounded up to whole rounds of keys, are 32-bit numbers.  (For a batch that validate_batch passed.)
+inline bool lengths_fit(const cs_batch* batch) {
+    for (int32_t s = 0; s < batch->num_seqs; ++s)
+        if ((int64_t)batch->h_ctx_lens[s] + batch->h_cu_q_lens[s + 1] - batch->h_cu_q_lens[s] > 0x7fffffffll - 4096) return false;
+    return true;
+}
 
 // Split arithmetic of the decode path, shared by the host plan and the kernels.  A decode
 // sequence with n keys is cut into round(n / split) pieces (at least one) of equal,

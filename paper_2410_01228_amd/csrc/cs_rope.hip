@@ -434,6 +434,7 @@ static int append_rope(const cs_kv_pool* pool, int32_t layer, const cs_batch* ba
     rc = validate_batch(pool, batch);
     if (rc) return rc;
     if (batch->num_tokens == 0) return CS_OK;
+    if (!lengths_fit(batch)) return CS_ERR_UNSUPPORTED;
     RopeArgs a;
     const int32_t Hkv = pool->num_kv_heads, D = pool->head_dim;
     rc = fill_rope(rope, q, q_stride, k, k_stride, q_out, batch->num_tokens, Hq, Hkv, D, true, a);

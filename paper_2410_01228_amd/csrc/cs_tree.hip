@@ -35,16 +35,17 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
     p.tiles = most <= 1 ? 1 : most <= 2 ? most : (most + 3) / 4 * 4;
     // Pieces: the length at which a model of the launch ends first.  Workgroups of the chip's slots take the pieces in order, the longest first;
     // a step costs what it does on a full chip (measured with 512 workgroups of 4064 and 8160 keys, 8 kv heads), and a piece of a cut sequence its partial
-    // result and a share of the merge.  (Halving from 8192 until there were two workgroups a CU, whatever their lengths: FIT.)
+    // result and a share of the merge.  (A fixed rule, halving from 8192 keys until there were two
+    // workgroups a CU: 705 us where this one has 543, 8 trees of 64 nodes and 8 heads on 2K-32K keys.)
     const int32_t slots = std::max(1, device_cus() * (p.tiles == 2 && D == 128 ? 1 : 2) / Hkv);
     auto step_us = [&](int32_t tiles) {
         const double us = tiles <= 2 ? 1.25 : tiles <= 8 ? 1.32 : 1.72;
         return (D == 64 ? (tiles <= 2 ? 0.5 : 0.6) : p.tiles == 2 ? 0.5 : 1.0) * us;
     };
-    auto pieces_of = [&](int32_t s, int32_t split) {
+    auto pieces_of = [&](int32_t s, int64_t split) {
         const int32_t q = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s], n = b->h_ctx_lens[s] + q, blocks = tree_blocks(q * G).blocks;
         if (blocks == 0) return 0;
-        int32_t k = std::min(std::max((n + split / 2) / split, 1), std::min(kTreeMaxPieces, kMaxArgItems / blocks));
+        int32_t k = std::min(std::max((int32_t)((n + split / 2) / split), 1), std::min(kTreeMaxPieces, kMaxArgItems / blocks));
         for (int32_t fewer = k; k > 1; k = fewer) {              // (rounding a piece's length up can leave the last one empty)
             const int32_t c = tree_chunk_keys(n, k);
             fewer = (n + c - 1) / c;
@@ -52,14 +53,14 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
         }
         return k;
     };
-    int32_t longest = 1;
+    int64_t longest = kTreeLeastPiece;
     for (int32_t s = 0; s < S; ++s)
-        if (b->h_cu_q_lens[s + 1] > b->h_cu_q_lens[s]) longest = std::max(longest, b->h_ctx_lens[s] + b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s]);
-    int32_t split = 2 * longest;                                 // (nothing is cut)
+        if (b->h_cu_q_lens[s + 1] > b->h_cu_q_lens[s]) longest = std::max<int64_t>(longest, b->h_ctx_lens[s] + b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s]);
+    const int64_t whole = 2 * longest;                           // nothing is cut
+    int64_t split = whole;
     double least = 0;
     std::vector<float> work, busy;
-    for (int32_t trial = 2 * longest; ; trial = trial == 2 * longest ? std::max(longest, kTreeLeastPiece) : trial * 4 / 5) {
-        if (trial < kTreeLeastPiece) break;
+    for (int64_t trial = whole; trial >= kTreeLeastPiece; trial = trial == whole ? longest : trial * 4 / 5) {
         work.clear();
         double partials = 0;
         for (int32_t s = 0; s < S; ++s) {
@@ -73,7 +74,7 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
             }
             if (k > 1) partials += (double)k * t.blocks * t.tiles;
         }
-        if ((int64_t)work.size() > kTreeModelled && trial != 2 * longest) break;    // (pieces enough for an even end)
+        if ((int64_t)work.size() > kTreeModelled && trial != whole) break;    // (pieces enough for an even end)
         std::sort(work.begin(), work.end(), std::greater<float>());
         busy.assign(slots, 0.f);                                 // a heap of when the slots come free
         for (float w : work) {
@@ -83,7 +84,7 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
         }
         double end = *std::max_element(busy.begin(), busy.end());
         if (partials > 0) end += 4.0 + partials * Hkv * 16 * D * 8 / 5e6;
-        if (trial == 2 * longest || end < least) { least = end; split = trial; }
+        if (trial == whole || end < least) { least = end; split = trial; }
     }
     struct Seq { int32_t seq, pieces, blocks, keys; };
     std::vector<Seq> seqs;
@@ -187,7 +188,7 @@ static int attention_tree(const cs_kv_pool* pool, int32_t layer, const cs_batch*
     if (rc) return rc;
     if (batch->num_tokens == 0) return CS_OK;
     const int32_t most = most_new(batch);
-    if (most > CS_MAX_TREE) return CS_ERR_UNSUPPORTED;
+    if (most > CS_MAX_TREE || !lengths_fit(batch)) return CS_ERR_UNSUPPORTED;
     if (!q || !out || ((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return CS_ERR_INVALID_ARG;
     if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return CS_ERR_INVALID_ARG;   // positive, finite
     if (mask && (((uintptr_t)mask & 7) || mask_words < (most + 63) / 64 || mask_words > kTreeWords)) return CS_ERR_INVALID_ARG;
@@ -217,7 +218,7 @@ extern "C" {
 
 size_t cs_paged_attention_tree_workspace_bytes(const cs_batch* batch, int32_t Hq, int32_t Hkv, int32_t D) {
     if (attention_shape_ok(Hq, Hkv, D) != CS_OK) return 0;
-    if (validate_batch(nullptr, batch) != CS_OK || batch->num_seqs == 0 || most_new(batch) > CS_MAX_TREE) return 0;
+    if (validate_batch(nullptr, batch) != CS_OK || batch->num_seqs == 0 || most_new(batch) > CS_MAX_TREE || !lengths_fit(batch)) return 0;
     try { return tree_plan_for(batch, Hq, Hkv, D).bytes; } catch (const std::bad_alloc&) { return 0; }
 }
 

@@ -10,6 +10,7 @@
 // (sequence, kv head, key range, block of up to 192 rows), its wavefronts take 32-key steps in turn.  Bound by HBM up to some 128 rows a kv
 // head and beyond that by the matrix unit and the softmax's vector instructions.
 #pragma once
+#include <type_traits>
 #include "cs_decode_impl.h"
 #include "cs_prefill_impl.h"
 #include "cs_tree.h"
@@ -402,9 +403,10 @@ __global__ __launch_bounds__(kDecodeThreads, (tree_waves(D, NC))) void tree_kern
 
 // ------------------------------------------------------------------------------------
 // More than two column tiles: the wavefronts share the rows instead of the keys.  A step's K and V are copied into an LDS ring by
-// LDS-DMA, three steps ahead of the one that is multiplied, and every wavefront reads them from there for its one or two tiles; Q stays
+// LDS-DMA, three steps ahead of the one that is multiplied, and every wavefront reads them from there for its one to three tiles; Q stays
 // in registers.  (With the keys dealt to the wavefronts, as above, eight tiles' outputs leave registers for one step of K and V only,
-// whose loads then wait for the step before: 64 tokens of 8 heads on contexts of 2K-32K keys took 845 us of a batch that this form does in RING us.)
+// whose loads then wait for the step before: 8 trees of 64 nodes and
+// 8 heads on contexts of 2K-32K keys: 1173 us in that form, 543 in this one, whose copies and plan are the better for it too.)
 //
 // LDS arrangement of a step: K block of the first 16-key step, 64 bytes, K block of the second, the V blocks; each as in a page of
 // 16 tokens.  Row r = 8 * step + 4 * half + i of score tile X (Y) is token 8 * half + i (+ 4) of its step, so that over X and Y a lane group

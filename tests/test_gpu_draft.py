@@ -353,6 +353,43 @@ def test_what_a_row_does_not_see_has_no_effect_on_it(what, dtype):
                 assert torch.all(row[4:] == (float("inf") if "-" not in what else float("-inf")))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("page_size", [16, 8])
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_number_of_row_tiles(D, page_size, dtype):
+    """Rows that fill 1 to 27 tiles of 16, the last one partly, beside a sequence with fewer; contexts from none to some rounds of keys."""
+    G, rng = 5, np.random.default_rng(31)
+    for tiles in range(1, 28):
+        n = -(-(16 * (tiles - 1) + 1) // G)
+        ctx, new = (int(rng.integers(0, 600)), int(rng.integers(0, 300))), (n, int(rng.integers(0, n + 1)))
+        w = World(ctx, new, 1, D, tiles, dtype, page_size)
+        q = tree_step(w, G, w.rng)
+        masks = [draft.ancestors(random_tree(w.rng, m, 6)) if m else np.zeros((0, 1), bool) for m in new]
+        check_tree(w, q, G, masks, D ** -0.5, run_tree(w, q, G, masks, D ** -0.5))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("page_size", [16, 8])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nodes", [3, 7, 10, 20, 40])
+def test_long_walks_over_shared_pages(nodes, D, page_size, dtype):
+    """As many sequences as the chip has room for, so that none is cut, all behind one prefix whose page table is longer than a wavefront."""
+    S, ctx, Hkv, Hq, pages = 16, 1216, 32, 128, 1216 // page_size
+    w = World([ctx] + [0] * (S - 1), [nodes] * S, Hkv, D, nodes, dtype, page_size)
+    own = w.tables[1:, :w.tables.shape[1] - pages].copy()
+    w.tables[1:, :pages] = w.tables[0, :pages]
+    w.tables[1:, pages:] = own
+    w.ctx = [ctx] * S
+    q = tree_step(w, Hq, w.rng)
+    masks = [draft.ancestors(random_tree(w.rng, nodes, 3)) for _ in range(S)]
+    got = run_tree(w, q, Hq, masks, D ** -0.5)
+    for s in (0, 7, 15):
+        k, v = w.logical(s)
+        t0 = s * nodes
+        want, tol = draft.ref_tree_attention(q[t0:t0 + nodes].double().numpy(), k, v, masks[s], D ** -0.5, HALF_STEP[dtype], dtype == F16)
+        near(got[t0:t0 + nodes].double().numpy(), want, tol, s)
+
+
 def test_trees_agree_with_the_mixed_call_on_chains_and_tokens():
     Hq, Hkv, D, ctx, new = 32, 8, 128, (100, 900, 33, 0), (1, 6, 40, 3)
     w = World(ctx, new, Hkv, D, 25)
