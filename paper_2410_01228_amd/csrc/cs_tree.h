@@ -8,16 +8,17 @@ constexpr int kTreeWords = CS_MAX_TREE / 64;                     // mask words o
 constexpr int kTreeTiles = 12;                                   // column tiles (16 rows) of a workgroup at most: three a wavefront
 
 // The column tiles of R = nodes * G rows, dealt evenly to workgroups.  One or two tiles are a workgroup whose wavefronts share the keys.  Otherwise a
-// wavefront has one to three of them, and a workgroup's time goes by its fullest wavefront: the number that leaves the least of
-// four times as many empty is taken, the larger one where they are even (K and V are read once for all of them).
+// wavefront has one to three of them.  A step of a workgroup whose fullest wavefront has n tiles takes n + 1 units (0.70, 0.98 and 1.32 us of 512
+// workgroups at D = 128, with four and more blocks of a sequence; 0.35, 0.56 and 0.79 at D = 64): the n with the least of them in all blocks is
+// taken.  (Not the one with the fewest tiles missing, n units a step: 48 sequences of 28 tiles on 4K keys, 7 blocks with n = 1, 559 us, 4 with n = 2, 388.)
 struct TreeBlocks { int32_t blocks, tiles; };
 __host__ __device__ inline TreeBlocks tree_blocks(int32_t rows) {
     const int32_t all = (rows + 15) / 16;
     if (all <= 2) return {all > 0 ? 1 : 0, all};
-    int32_t best = 1, least = (all + 3) / 4;
+    int32_t best = 1, least = (all + 3) / 4 * 2;
     for (int32_t each = 2; each <= 3; ++each) {
-        const int32_t cost = (all + 4 * each - 1) / (4 * each) * each;
-        if (cost <= least) { least = cost; best = each; }
+        const int32_t cost = (all + 4 * each - 1) / (4 * each) * (each + 1);
+        if (cost < least) { least = cost; best = each; }
     }
     const int32_t blocks = (all + 4 * best - 1) / (4 * best);
     return {blocks, (all + blocks - 1) / blocks};

@@ -38,9 +38,10 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
     // result and a share of the merge.  (A fixed rule, halving from 8192 keys until there were two
     // workgroups a CU: 705 us where this one has 543, 8 trees of 64 nodes and 8 heads on 2K-32K keys.)
     const int32_t slots = std::max(1, device_cus() * (p.tiles == 2 && D == 128 ? 1 : 2) / Hkv);
-    auto step_us = [&](int32_t tiles) {
-        const double us = tiles <= 2 ? 1.25 : tiles <= 8 ? 1.32 : 1.72;
-        return (D == 64 ? (tiles <= 2 ? 0.5 : 0.6) : p.tiles == 2 ? 0.5 : 1.0) * us;
+    auto step_us = [&](const TreeBlocks& t) {
+        if (p.tiles <= 2) return 1.25 * (D == 64 || p.tiles == 2 ? 0.5 : 1.0);
+        const double bytes = 1.31 / t.blocks, products = 0.33 * ((t.tiles + 3) / 4 + 1);   // a sequence's blocks share what they read
+        return (D == 64 ? 0.55 : 1.0) * std::max(bytes, products + 0.22 * bytes);
     };
     auto pieces_of = [&](int32_t s, int64_t split) {
         const int32_t q = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s], n = b->h_ctx_lens[s] + q, blocks = tree_blocks(q * G).blocks;
@@ -70,7 +71,7 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
             const int32_t chunk = tree_chunk_keys(n, k);
             for (int32_t i = 0; i < k; ++i) {
                 const int32_t keys = std::min(chunk, n - i * chunk);
-                for (int32_t j = 0; j < t.blocks; ++j) work.push_back((float)(8.0 + (keys + 31) / 32 * step_us(t.tiles)));
+                for (int32_t j = 0; j < t.blocks; ++j) work.push_back((float)(8.0 + (keys + 31) / 32 * step_us(t)));
             }
             if (k > 1) partials += (double)k * t.blocks * t.tiles;
         }
