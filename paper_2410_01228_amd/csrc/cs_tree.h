@@ -43,5 +43,8 @@ struct TreeItems {
     int32_t base;                                                // number of the first item, of all the call's
     uint32_t e[kMaxArgItems];
 };
+struct TreeMerges {                                              // the first pieces of cut blocks: word, and number of all the call's
+    struct { uint32_t word; int32_t item; } e[kMaxArgItems / 2];
+};
 
 }  // namespace cs

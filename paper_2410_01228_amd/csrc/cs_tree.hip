@@ -164,9 +164,15 @@ static int run_tree(const TreePlan& p, const cs_kv_pool& pool, int32_t layer, co
         const float f = scale * 1.44269504088896340736f;
         if (pool.page_size == 16) launch_tree<D, E, 16>(p, pool, layer_base, b, G, mask, mask_words, q, out, f, part, items, n, st);
         else                      launch_tree<D, E, 8>(p, pool, layer_base, b, G, mask, mask_words, q, out, f, part, items, n, st);
-        if (p.cut)
-            hipLaunchKernelGGL((tree_merge_kernel<D, E>), dim3((uint32_t)n * (uint32_t)pool.num_kv_heads, (uint32_t)p.tiles), dim3(kDecodeThreads), 0, st,
-                               pool.num_kv_heads, G, 16 * p.tiles, b.cu_q_lens, out, part, items);
+        TreeMerges merges;
+        uint32_t cut = 0;
+        for (int32_t j = 0; p.cut && j < n; ++j) {
+            const TreeItem it = tree_item(items.e[j]);
+            if (it.pieces > 1 && it.piece == 0) merges.e[cut++] = {items.e[j], items.base + j};
+        }
+        if (cut > 0)
+            hipLaunchKernelGGL((tree_merge_kernel<D, E>), dim3(cut * (uint32_t)pool.num_kv_heads, (uint32_t)p.tiles), dim3(4 * D), 0, st,
+                               pool.num_kv_heads, G, 16 * p.tiles, b.cu_q_lens, out, part, merges);
     }
     return check_launch("tree_kernel");
 }

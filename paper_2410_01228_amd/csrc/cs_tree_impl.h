@@ -650,58 +650,55 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
     }
 }
 
-// Joins the pieces of cut blocks: a workgroup for each column tile (grid.y) of each first piece and kv head, a thread for 4 features of a row.
+// Joins the pieces of cut blocks: a workgroup for each column tile (grid.y) of each cut block and kv head, a thread for 4 features of a row.
 template <int D, class E>
-__global__ __launch_bounds__(kDecodeThreads) void tree_merge_kernel(
-    int32_t Hkv, int32_t G, int32_t part_rows, const int32_t* __restrict__ cu_q_lens, uint16_t* __restrict__ out, TreePartials part, const TreeItems items)
+__global__ __launch_bounds__(4 * D) void tree_merge_kernel(
+    int32_t Hkv, int32_t G, int32_t part_rows, const int32_t* __restrict__ cu_q_lens, uint16_t* __restrict__ out, TreePartials part, const TreeMerges merges)
 {
-    const int32_t item = (int32_t)blockIdx.x / Hkv, g = (int32_t)blockIdx.x - item * Hkv, c = blockIdx.y;
-    const TreeItem it = tree_item(items.e[item]);
-    if (it.pieces == 1 || it.piece != 0) return;
+    const int32_t merge = (int32_t)blockIdx.x / Hkv, g = (int32_t)blockIdx.x - merge * Hkv, c = blockIdx.y;
+    const TreeItem it = tree_item(merges.e[merge].word);
     const int32_t t0 = cu_q_lens[it.seq], rows = (cu_q_lens[it.seq + 1] - t0) * G, Hq = Hkv * G;
     const TreeBlocks blocks = tree_blocks(rows);
     if (c >= blocks.tiles) return;
-    for (int32_t u = threadIdx.x; u < 16 * (D / 4); u += kDecodeThreads) {
-        const int32_t r = u / (D / 4), d = (u - r * (D / 4)) * 4, row = (it.block * blocks.tiles + c) * 16 + r;
-        if (row >= rows) continue;
-        float M = -INFINITY, L = 0.f;
-        f32x4 O = {0.f, 0.f, 0.f, 0.f};
-        const int64_t at = ((int64_t)(items.base + item) * Hkv + g) * part_rows + c * 16 + r, next = (int64_t)blocks.blocks * Hkv * part_rows;
-        // eight pieces' loads in flight at once; with more of them the maxima are read twice
-        for (int32_t i0 = 0; it.pieces > 8 && i0 < it.pieces; i0 += 8) {
-            float m[8];
+    const int32_t r = (int32_t)threadIdx.x / (D / 4), d = ((int32_t)threadIdx.x - r * (D / 4)) * 4, row = (it.block * blocks.tiles + c) * 16 + r;
+    if (row >= rows) return;
+    float M = -INFINITY, L = 0.f;
+    f32x4 O = {0.f, 0.f, 0.f, 0.f};
+    const int64_t at = ((int64_t)merges.e[merge].item * Hkv + g) * part_rows + c * 16 + r, next = (int64_t)blocks.blocks * Hkv * part_rows;
+    // eight pieces' loads in flight at once; with more of them the maxima are read twice
+    for (int32_t i0 = 0; it.pieces > 8 && i0 < it.pieces; i0 += 8) {
+        float m[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m[i] = part.ml[(at + min(i0 + i, it.pieces - 1) * next) * 2];
+        for (int i = 0; i < 8; ++i) m[i] = part.ml[(at + min(i0 + i, it.pieces - 1) * next) * 2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) M = fmaxf(M, m[i]);
-        }
-        for (int32_t i0 = 0; i0 < it.pieces; i0 += 8) {
-            typedef float f32x2 __attribute__((ext_vector_type(2)));
-            f32x2 ml[8];
-            f32x4 o[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {                        // (past the last piece: the last again)
-                const int64_t p = at + min(i0 + i, it.pieces - 1) * next;
-                ml[i] = *(const f32x2*)(part.ml + p * 2);
-                o[i] = *(const f32x4*)(part.o + p * D + d);
-            }
-            if (it.pieces <= 8) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) M = fmaxf(M, ml[i][0]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (i0 + i >= it.pieces || (ml[i][0] == -INFINITY && ml[i][1] == 0.f)) continue;     // (not a weight of zero: an infinity in V stays one)
-                const float f = exp2f(ml[i][0] - M);
-                L += ml[i][1] * f;
-                O += o[i] * f;
-            }
-        }
-        const int32_t node = row / G, head = row - node * G;
-        u32x2 w = {0u, 0u};
-        if (L != 0.f) w = u32x2{ E::pack(O[0] / L, O[1] / L), E::pack(O[2] / L, O[3] / L) };
-        *(u32x2*)(out + ((int64_t)(t0 + node) * Hq + g * G + head) * D + d) = w;
+        for (int i = 0; i < 8; ++i) M = fmaxf(M, m[i]);
     }
+    for (int32_t i0 = 0; i0 < it.pieces; i0 += 8) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        f32x2 ml[8];
+        f32x4 o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {                        // (past the last piece: the last again)
+            const int64_t p = at + min(i0 + i, it.pieces - 1) * next;
+            ml[i] = *(const f32x2*)(part.ml + p * 2);
+            o[i] = *(const f32x4*)(part.o + p * D + d);
+        }
+        if (it.pieces <= 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) M = fmaxf(M, ml[i][0]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i0 + i >= it.pieces || (ml[i][0] == -INFINITY && ml[i][1] == 0.f)) continue;     // (not a weight of zero: an infinity in V stays one)
+            const float f = exp2f(ml[i][0] - M);
+            L += ml[i][1] * f;
+            O += o[i] * f;
+        }
+    }
+    const int32_t node = row / G, head = row - node * G;
+    u32x2 w = {0u, 0u};
+    if (L != 0.f) w = u32x2{ E::pack(O[0] / L, O[1] / L), E::pack(O[2] / L, O[3] / L) };
+    *(u32x2*)(out + ((int64_t)(t0 + node) * Hq + g * G + head) * D + d) = w;
 }
 
 }  // namespace cs
