@@ -539,7 +539,8 @@ int cs_kv_append_rope_f16(const cs_kv_pool* pool, int32_t layer, const cs_batch*
  * CS_MAX_TREE / 64; NULL: nodes 0 .. i (a chain).  Any mask will do; a row that sees no key at all is zeros.  What lies
  * in K or V of a key that a row does not see has no effect on it, infinities and NaN among it.  Bits of nodes that the
  * sequence does not have are not looked at.  Everything else is as in cs_paged_attention_mixed (a single token is a tree of
- * one node); chunks of more than CS_MAX_TREE tokens are CS_ERR_UNSUPPORTED.  workspace: at least
+ * one node); chunks of more than CS_MAX_TREE tokens, and positions from 2^31 - 4096 on (here, in
+ * cs_kv_append_rope and in cs_kv_tree_commit), are CS_ERR_UNSUPPORTED.  workspace: at least
  * cs_paged_attention_tree_workspace_bytes(), 0 for many batches; contents are scratch, and calls that overlap in
  * time need one each. */
 size_t cs_paged_attention_tree_workspace_bytes(const cs_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim);
@@ -561,7 +562,8 @@ int cs_paged_attention_tree_f16(const cs_kv_pool* pool, int32_t layer, const cs_
  * or no number counts as 0; a token outside the vocabulary is refused.
  *   tokens, parents, u: device [T], entries of node 0 not read; parents[i] < i, in the sequence's own numbers (a node whose parent
  *   is none of 0 .. i - 1 is never reached), NULL: a chain.  p, q: device fp32, the row of token t from p + t * p_stride on
- *   (strides in elements, >= vocab); the distribution behind t, and the one that t's children were drawn from.
+ *   (strides in elements, >= vocab); the distribution behind t, and the one that t's children were drawn from (not read where
+ *   t has none).
  *   u_next: device [S].
  *   out_tokens[cu_q_lens[s] + k]: the tokens that the step brings, k < count[s], then -1;  path[..]: their nodes' numbers, node 0 first
  *   (token k follows node path[k]), then -1;  count: device [S], accepted drafts + 1; 0 for a sequence without new tokens.

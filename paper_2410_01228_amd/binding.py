@@ -701,7 +701,7 @@ def _head_rows(t: torch.Tensor, tokens: int, heads: int, D: int):
     """(address, elements between tokens) of a [tokens, heads, D] tensor whose tokens may lie apart."""
     n, h, d = t.shape
     step, b, c = t.stride()
-    assert n >= tokens and h == heads and d == D == b and c == 1 and t.dtype in _16_BITS
+    assert n >= tokens and h == heads and d == D and (b == D or h == 1) and c == 1 and t.dtype in _16_BITS
     return t.data_ptr(), step if n > 1 else h * d
 
 

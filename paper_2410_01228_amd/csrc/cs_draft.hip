@@ -143,7 +143,7 @@ __device__ __forceinline__ void walk(const Nodes& d, VerifyLds& s, int32_t node,
     if (lane == 0) { s.node = node; s.last = last; s.c = c; s.z = z; s.done = done; s.len = len; s.refused = refused; }
 }
 
-// Four consecutive elements of what is left of a row, zeros behind its end.
+// Four consecutive elements of a row's p and q, zeros behind its end.
 template <bool kDrawn>
 __device__ __forceinline__ void load_left(const float* __restrict__ p, const float* __restrict__ q, int32_t at, int32_t vocab, float (&x)[4], float (&y)[4])
 {
@@ -334,8 +334,10 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
         walk<kDrawn>(d, s, 0, 0, 0.0, 1.0, 1, lane);
     }
     __syncthreads();
-    const float* p = a.p + (int64_t)(t0 + s.node) * a.p_stride;
-    const float* q = kDrawn ? a.q + (int64_t)(t0 + s.node) * a.q_stride : nullptr;
+    // The node's rows.  Where no child was refused nobody has to have filled q's (a leaf has none): p's stands in, 0 times it is taken off.
+    auto row_p = [&] { return a.p + (int64_t)(t0 + __builtin_amdgcn_readfirstlane(s.node)) * a.p_stride; };
+    auto row_q = [&] { return kDrawn && __builtin_amdgcn_readfirstlane(s.c != 0.0) ? a.q + (int64_t)(t0 + __builtin_amdgcn_readfirstlane(s.node)) * a.q_stride : row_p(); };
+    const float *p = row_p(), *q = row_q();
     double* sums = a.sums + (int64_t)seq * a.blocks;
     block_sums<kDrawn>(s, p, q, s.c, part * kVerifyWaves + wave, a.parts * kVerifyWaves, a.blocks, a.vocab, lane, [&](int32_t b, double v) {
         if (lane == 0) {
@@ -377,8 +379,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
         }
         __syncthreads();
         if (s.merges) break;
-        p = a.p + (int64_t)(t0 + s.node) * a.p_stride;
-        if (kDrawn) q = a.q + (int64_t)(t0 + s.node) * a.q_stride;
+        p = row_p();
+        q = row_q();
         block_sums<kDrawn>(s, p, q, s.c, wave, kVerifyWaves, a.blocks, a.vocab, lane, [&](int32_t b, double v) {
             if (lane == 0) s.sums[b] = v;
         });

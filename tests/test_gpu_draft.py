@@ -567,6 +567,18 @@ def test_verification_of_rows_with_little_in_them(drawn):
     d.check(args)
 
 
+@pytest.mark.parametrize("vocab", [900, 50257])
+def test_verification_leaves_unread_what_a_leaf_has_no_drafts_from(vocab):
+    """Rows of q behind nodes without children were never filled; neither were rows of p that no walk reaches."""
+    d = Drafts((6, 1, 30, 2), vocab, True, 58)
+    leaf = np.ones(len(d.tokens), bool)
+    for s, n in enumerate(d.new):
+        leaf[[d.cu[s] + p for p in d.parents[d.cu[s] + 1:d.cu[s] + n]]] = False
+    d.u[::2] = 0.0                                                # walks that end at leaves
+    d.q[leaf] = np.nan
+    assert max(d.run()) > 2
+
+
 # ------------------------------------------------------------------------------------ commit
 
 @pytest.mark.parametrize("page_size", [16, 8])
