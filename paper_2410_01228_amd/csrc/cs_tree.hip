@@ -49,7 +49,7 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
         int32_t k = std::min(std::max((int32_t)((n + split / 2) / split), 1), std::min(kTreeMaxPieces, kMaxArgItems / blocks));
         for (int32_t fewer = k; k > 1; k = fewer) {              // (rounding a piece's length up can leave the last one empty)
             const int32_t c = tree_chunk_keys(n, k);
-            fewer = (n + c - 1) / c;
+            fewer = (int32_t)(((int64_t)n + c - 1) / c);
             if (fewer >= k) break;
         }
         return k;

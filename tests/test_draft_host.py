@@ -192,6 +192,35 @@ def test_commit_refused():
     assert _commit(l0=1, l1=1) == cs.CS_OK and _commit(batch=_batch((1,), (0,))) == cs.CS_OK
 
 
+def test_far_positions_refused():
+    """Positions, rounded up to a workgroup's keys, are 32-bit numbers."""
+    far = lambda c: _batch((5, c), (1, 3), 2 ** 28)  # noqa: E731
+    ask = lambda b: cs.lib().cs_paged_attention_tree_workspace_bytes(ctypes.byref(b), 4, 2, 64)  # noqa: E731
+    last = 2 ** 31 - 1 - 4096 - 3
+    for c in (last + 1, 2 ** 31 - 4, 2 ** 31 - 1):
+        assert _append(_rope(), batch=far(c)) == UNS and _tree(batch=far(c)) == UNS and _commit(batch=far(c)) == UNS and ask(far(c)) == 0
+    # the last one that is taken is planned for: it is cut, so a call without room for the pieces is refused
+    assert 0 < ask(far(last)) < 1 << 30 and _tree(batch=far(last), wb=16) == SMALL
+
+
+def test_threads_plan_for_themselves():
+    import threading
+    batches = [_batch((20000 + 100 * i, 7), (1 + i, 5), 4000) for i in range(12)]
+    ask = lambda b: cs.lib().cs_paged_attention_tree_workspace_bytes(ctypes.byref(b), 8, 2, 128)  # noqa: E731
+    want, wrong = [ask(b) for b in batches], []
+
+    def work(seed):
+        for i in np.random.default_rng(seed).integers(0, 12, 400):
+            if ask(batches[i]) != want[i]:
+                wrong.append(i)
+    threads = [threading.Thread(target=work, args=(s,)) for s in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(set(want)) > 1 and not wrong
+
+
 def test_binding_refuses_views_that_the_calls_would_read_past():
     inv, pos = torch.ones(32), torch.arange(7, dtype=torch.int32)
     q, k = torch.zeros(7, 4, 64, dtype=torch.bfloat16), torch.zeros(7, 2, 64, dtype=torch.bfloat16)

@@ -705,19 +705,22 @@ def test_steps_of_speculation_leave_the_cache_of_plain_decoding(dtype):
 
 # -------------------------------------------------------------------- streams, graphs, repetition
 
-def all_calls(seed, capture_ws=True):
-    """One step's five calls on prepared memory, and its outputs."""
+def all_calls(seed, like=None):
+    """One step's five calls on prepared memory, and its outputs.  like: another one's, whose workspaces it takes."""
     w = World((2500, 40, 9), (12, 5, 1), 2, 64, seed)
     rng = w.rng
     rope, _, _, _ = make_rope(rng, w.T, 64, 64, False, True, 1, BF16)
     x = torch.from_numpy(rng.standard_normal((w.T, 12, 64))).to(BF16).cuda()
     pool, t = w.device_pool()
     batch, q_out, k_out = w.batch(), torch.zeros((w.T, 8, 64), dtype=BF16, device="cuda"), torch.zeros((w.T, 2, 64), dtype=BF16, device="cuda")
-    out, ws = torch.zeros_like(q_out), cs.workspace_for_tree(batch, 8, 2, 64)
-    ws.fill_(255)
+    out, ws = torch.zeros_like(q_out), cs.workspace_for_tree(batch, 8, 2, 64) if like is None else like[2][4]
+    if like is None:
+        ws.fill_(255)
     mask = torch.from_numpy(np.concatenate([draft.mask_words(draft.ancestors(random_tree(rng, n, 3)), 1) for n in w.new])).cuda()
-    d = Drafts(w.new, 9000, True, seed)
+    d = Drafts(w.new, 40000, True, seed)                          # (rows that several workgroups sum)
     v = d.device()
+    if like is not None:
+        v[10] = like[2][3][10]
 
     def step():
         cs.cs_qk_rope(rope, x[:, :8], x[:, 8:10], q_out, k_out)
@@ -725,7 +728,7 @@ def all_calls(seed, capture_ws=True):
         cs.cs_paged_attention_tree(pool, 0, batch, q_out, out, 8, 0.125, mask, ws)
         cs.cs_spec_verify(*v)
         cs.cs_kv_tree_commit(pool, 0, 1, batch, v[8], v[9])
-    return step, [q_out, k_out, out, v[7][:w.T], v[8][:w.T], v[9][:3], t], (w, batch, d, v)
+    return step, [q_out, k_out, out, v[7][:w.T], v[8][:w.T], v[9][:3], t], (w, batch, d, v, ws)
 
 
 def clear(outs):
@@ -751,6 +754,26 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
     keep[2].check(keep[3])
+
+
+def test_two_graphs_that_share_their_workspaces():
+    first = all_calls(85)
+    runs = [first, all_calls(86, first)]
+    want, graphs = [], []
+    for step, outs, _ in runs:
+        step()
+        torch.cuda.synchronize()
+        want.append([o.clone() for o in outs])
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            step()
+    for i in (0, 1, 1, 0, 0, 1, 0, 1):
+        clear(runs[i][1])
+        graphs[i].replay()
+        runs[1 - i][0]()                                          # and the other one's calls behind it
+        torch.cuda.synchronize()
+        for (_, outs, _), w in zip(runs, want):
+            assert all(torch.equal(a, b) for a, b in zip(outs, w))
 
 
 def test_two_streams_at_once():
