@@ -202,6 +202,29 @@ __device__ __forceinline__ double wave_sum(double v) {
     return join(lo[0], hi[0]) + join(lo[1], hi[1]);
 }
 
+// Sums over the lanes up to each one (the same way).
+__device__ __forceinline__ double wave_scan(double v) {
+    auto add = [&](auto ctrl, auto rows) {
+        constexpr int c = decltype(ctrl)::value, r = decltype(rows)::value;
+        const uint64_t w = __builtin_bit_cast(uint64_t, v);      // (lanes without a source, or outside the rows: 0)
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, c, r, 0xf, false);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), c, r, 0xf, false);
+        v += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    };
+    typedef std::integral_constant<int, 0xf> All;
+    add(std::integral_constant<int, 0x111>{}, All{});            // 1, 2, 4, 8 lanes up within 16
+    add(std::integral_constant<int, 0x112>{}, All{});
+    add(std::integral_constant<int, 0x114>{}, All{});
+    add(std::integral_constant<int, 0x118>{}, All{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // lane 15 (47) to the 16 lanes behind it
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // lane 31 to the 32 behind it
+    return v;
+}
+__device__ __forceinline__ double lane_of(double v, int32_t lane) {
+    const uint64_t w = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)lane_of((int32_t)(w >> 32), lane) << 32 | (uint64_t)(uint32_t)lane_of((int32_t)(uint32_t)w, lane));
+}
+
 template <bool kDrawn>
 __device__ __forceinline__ void load_block(const VerifyLds& s, const float* p, const float* q, int32_t base, int32_t vocab, float (&x)[4][4], float (&y)[4][4], int lane)
 {
@@ -256,25 +279,20 @@ __device__ __forceinline__ int32_t draw_next(const VerifyArgs& a, const VerifyLd
     double at_block = 0.0, at_last = 0.0;
     for (int32_t b0 = 0; b0 < a.blocks; b0 += 64) {
         const double v = b0 + lane < a.blocks ? s.sums[b0 + lane] : 0.0;
-        double run = v;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const double o = __shfl_up(run, m, 64);
-            if (lane >= m) run += o;
-        }
+        const double run = wave_scan(v);
         const uint64_t some = __ballot(v > 0.0), pass = __ballot(v > 0.0 && before + run > target);
         if (some) {
             const int k = 63 - __builtin_clzll(some);
             last = b0 + k;
-            at_last = before + __shfl(run - v, k, 64);
+            at_last = before + lane_of(run - v, k);
         }
         if (pass) {
             const int k = __builtin_ctzll(pass);
             block = b0 + k;
-            at_block = before + __shfl(run - v, k, 64);
+            at_block = before + lane_of(run - v, k);
             break;
         }
-        before += __shfl(run, 63, 64);
+        before += lane_of(run, 63);
     }
     if (block < 0) { block = last; at_block = at_last; }         // (rounding, or u not below 1: the last one with anything left)
     if (block < 0) return -1;
@@ -287,12 +305,7 @@ __device__ __forceinline__ int32_t draw_next(const VerifyArgs& a, const VerifyLd
         double v[4], mine = 0.0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) { v[e] = left_of<kDrawn>(x[k][e], y[k][e], c); mine += v[e]; }
-        double run = mine;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const double o = __shfl_up(run, m, 64);
-            if (lane >= m) run += o;
-        }
+        const double run = wave_scan(mine);
         double at = before + (run - mine);
         int32_t hit = -1, held = -1;
 #pragma unroll
@@ -304,7 +317,7 @@ __device__ __forceinline__ int32_t draw_next(const VerifyArgs& a, const VerifyLd
         const uint64_t hits = __ballot(hit >= 0), helds = __ballot(held >= 0);
         if (token < 0 && hits) { const int l = __builtin_ctzll(hits); token = base + 4 * l + lane_of(hit, l); }
         if (helds) { const int l = 63 - __builtin_clzll(helds); some_token = base + 4 * l + lane_of(held, l); }
-        before += __shfl(run, 63, 64);
+        before += lane_of(run, 63);
     }
     return token >= 0 ? token : some_token;
 }
