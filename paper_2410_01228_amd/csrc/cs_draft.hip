@@ -143,39 +143,61 @@ __device__ __forceinline__ void walk(const Nodes& d, VerifyLds& s, int32_t node,
     if (lane == 0) { s.node = node; s.last = last; s.c = c; s.z = z; s.done = done; s.len = len; s.refused = refused; }
 }
 
-// Four consecutive elements of a row's p and q, zeros behind its end.
+// A lane's 16 elements of the 1024 from base on, 256 k + 4 lane .. + 3, of a row's p and q; zeros behind its end.  No branch stands between
+// the loads (each would be waited for at the next one): a quad across the end reads the row's last four elements and moves them into place.
 template <bool kDrawn>
-__device__ __forceinline__ void load_left(const float* __restrict__ p, const float* __restrict__ q, int32_t at, int32_t vocab, float (&x)[4], float (&y)[4])
+__device__ __forceinline__ void load_block(const float* __restrict__ p, const float* __restrict__ q, int32_t base, int32_t vocab, float (&x)[4][4], float (&y)[4][4], int lane)
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = y[i] = 0.f;
-    if (at + 4 <= vocab) {
-        const Quad a = *(const Quad*)(p + at);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = a.v[i];
-        if (kDrawn) {
-            const Quad b = *(const Quad*)(q + at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = b.v[i];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (at + i < vocab) { x[i] = p[at + i]; if (kDrawn) y[i] = q[at + i]; }
-    }
-}
-
-// Sets the refused guesses among elements base .. + 1024 of a lane's to nothing; lane l has base + 256 k + 4 l .. + 4.
-__device__ __forceinline__ void drop_refused(const VerifyLds& s, int32_t base, float (&x)[4][4], int lane)
-{
-    for (int32_t i = 0; i < s.refused; ++i) {
-        const int32_t at = s.gone[i] - base;
-        if (at < 0 || at >= kRowBlock) continue;
+    if (vocab < 4) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (at == 256 * k + 4 * lane + e) x[k][e] = 0.f;
+            for (int e = 0; e < 4; ++e) {
+                x[k][e] = y[k][e] = 0.f;
+                if (k == 0 && lane == 0 && e < vocab) { x[k][e] = p[e]; if (kDrawn) y[k][e] = q[e]; }
+            }
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int32_t at = min(base + 256 * k + 4 * lane, vocab - 4);
+        const Quad a = *(const Quad*)(p + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[k][e] = a.v[e];
+        if (kDrawn) {
+            const Quad b = *(const Quad*)(q + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[k][e] = b.v[e];
+        }
+    }
+    if (base + kRowBlock <= vocab) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int32_t past = base + 256 * k + 4 * lane - (vocab - 4);            // elements of the quad behind the end, if positive
+        auto place = [&](float (&v)[4]) {
+            if (past & 1 && past > 0) { v[0] = v[1]; v[1] = v[2]; v[2] = v[3]; }
+            if (past & 2 && past > 0) { v[0] = v[2]; v[1] = v[3]; }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = e + past < 4 ? v[e] : 0.f;
+        };
+        place(x[k]);
+        if (kDrawn) place(y[k]);
+    }
+}
+
+// Sets the refused guesses among a block's elements to nothing (arranged as by load_block).
+__device__ __forceinline__ void drop_refused(const VerifyLds& s, int32_t base, float (&x)[4][4], int lane)
+{
+    for (int32_t i0 = 0; i0 < s.refused; i0 += 64) {
+        const int32_t mine = i0 + lane < s.refused ? s.gone[i0 + lane] - base : -1;
+        for (uint64_t m = __ballot(mine >= 0 && mine < kRowBlock); m; m &= m - 1) {
+            const int32_t at = lane_of(mine, __builtin_ctzll(m));
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at == 256 * k + 4 * lane + e) x[k][e] = 0.f;
+        }
     }
 }
 
@@ -225,14 +247,6 @@ __device__ __forceinline__ double lane_of(double v, int32_t lane) {
     return __builtin_bit_cast(double, (uint64_t)(uint32_t)lane_of((int32_t)(w >> 32), lane) << 32 | (uint64_t)(uint32_t)lane_of((int32_t)(uint32_t)w, lane));
 }
 
-template <bool kDrawn>
-__device__ __forceinline__ void load_block(const VerifyLds& s, const float* p, const float* q, int32_t base, int32_t vocab, float (&x)[4][4], float (&y)[4][4], int lane)
-{
-#pragma unroll
-    for (int k = 0; k < 4; ++k) load_left<kDrawn>(p, q, base + 256 * k + 4 * lane, vocab, x[k], y[k]);
-    if (!kDrawn) drop_refused(s, base, x, lane);
-}
-
 // Sums of the blocks first, first + step, .. below end, by one wavefront; `take(block, sum)` gets them.  With drafts the next block is on its
 // way while one is summed: a node's refused children are passes by one workgroup, where nothing else hides the trip (4 trees of 64, 74 us
 // without).  Guesses have no such passes, and a block at a time is 1 us less for their short rows.
@@ -240,10 +254,7 @@ template <bool kDrawn, class Take>
 __device__ __forceinline__ void block_sums(const VerifyLds& s, const float* p, const float* q, double c, int32_t first, int32_t step, int32_t end, int32_t vocab, int lane, Take take)
 {
     float x[2][4][4], y[2][4][4];
-    auto load = [&](int32_t b, float (&xx)[4][4], float (&yy)[4][4]) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) load_left<kDrawn>(p, q, b * kRowBlock + 256 * k + 4 * lane, vocab, xx[k], yy[k]);
-    };
+    auto load = [&](int32_t b, float (&xx)[4][4], float (&yy)[4][4]) { load_block<kDrawn>(p, q, b * kRowBlock, vocab, xx, yy, lane); };
     auto sum = [&](int32_t b, float (&xx)[4][4], float (&yy)[4][4]) {
         if (!kDrawn) drop_refused(s, b * kRowBlock, xx, lane);
         double v = 0.0;
@@ -297,7 +308,8 @@ __device__ __forceinline__ int32_t draw_next(const VerifyArgs& a, const VerifyLd
     if (block < 0) { block = last; at_block = at_last; }         // (rounding, or u not below 1: the last one with anything left)
     if (block < 0) return -1;
     float x[4][4], y[4][4];
-    load_block<kDrawn>(s, p, q, block * kRowBlock, a.vocab, x, y, lane);
+    load_block<kDrawn>(p, q, block * kRowBlock, a.vocab, x, y, lane);
+    if (!kDrawn) drop_refused(s, block * kRowBlock, x, lane);
     int32_t token = -1, some_token = -1;
     before = at_block;
 #pragma unroll
