@@ -248,8 +248,8 @@ __device__ __forceinline__ double lane_of(double v, int32_t lane) {
 }
 
 // Sums of the blocks first, first + step, .. below end, by one wavefront; `take(block, sum)` gets them.  With drafts the next block is on its
-// way while one is summed: a node's refused children are passes by one workgroup, where nothing else hides the trip (4 trees of 64, 74 us
-// without).  Guesses have no such passes, and a block at a time is 1 us less for their short rows.
+// way while one is summed: a node's refused children are passes by one workgroup, where nothing else hides the trip (4 trees of 64: 74 us
+// without, 47 with).  Guesses have no such passes, and a block at a time is 1 us less for their short rows.
 template <bool kDrawn, class Take>
 __device__ __forceinline__ void block_sums(const VerifyLds& s, const float* p, const float* q, double c, int32_t first, int32_t step, int32_t end, int32_t vocab, int lane, Take take)
 {
@@ -439,7 +439,9 @@ static VerifyPlan plan_verify(int32_t S, int32_t vocab) {
 // ------------------------------------------------------------------------------------
 // Commit: K and V of path[k] go to slot ctx + k.  A path ascends and path[k] >= k, so a destination is never a later node's source:
 // a wavefront takes the nodes in order, eight at a time, and has read all eight before it writes any.
-// Bound by the cache lines that the page format spreads a token over, like the token copies of the checkpoint.
+// Bound by the cache lines that the page format spreads a token over, like the token copies of the checkpoint: 64 trees of 16-64 nodes, 32 layers of 8 heads
+// of 128, 44 us for 18 MB of rows that lie in 96 MB of lines read and 44 written.  A wavefront is a workgroup: four of them one, 10% slower;
+// K and V apart, 8% slower.
 // ------------------------------------------------------------------------------------
 constexpr int kCommitNodes = 8;
 

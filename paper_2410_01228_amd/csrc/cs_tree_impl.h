@@ -7,8 +7,8 @@
 //   O^T[d][row]  += V^T . P^T          v_mfma_f32_16x16x32, 32 keys: two steps' keys, four consecutive ones of either a lane group
 // with an online softmax per row in fp32.  K and V come from HBM into the operand registers as in decode (cs_decode_impl.h: the page
 // format is the operand layout), and each page read serves up to kTreeTiles column tiles: a workgroup is
-// (sequence, kv head, key range, block of up to 192 rows), its wavefronts take 32-key steps in turn.  Bound by HBM up to some 128 rows a kv
-// head and beyond that by the matrix unit and the softmax's vector instructions.
+// (sequence, kv head, key range, block of up to 192 rows), and its wavefronts take 32-key steps in turn (up to 32 rows) or rows (beyond).  Bound by HBM up
+// to some 128 rows a kv head, and beyond that by the matrix unit and the softmax's vector instructions at the clock that they leave the card.
 #pragma once
 #include <type_traits>
 #include "cs_decode_impl.h"
@@ -248,7 +248,8 @@ struct TreePartials {
     float *o, *ml;
 };
 
-// One or two column tiles: the wavefronts share the keys.
+// One or two column tiles: the wavefronts share the keys, each with the next step's K and V on their way into registers while it multiplies one.  Read once and
+// past the caches (4% faster than through them): 64 chains of 4-6 tokens on 512-4096, 32/8 heads, 100 us, 6.1 TB/s.
 template <int D, class E, int PS, int NC>
 __global__ __launch_bounds__(kDecodeThreads, (tree_waves(D, NC))) void tree_kernel(
     const uint16_t* __restrict__ layer_base, int64_t page_stride, int32_t num_pages, int32_t Hkv, int32_t G,

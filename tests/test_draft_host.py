@@ -3,6 +3,8 @@ would be enqueued."""
 import ctypes
 import os
 import re
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -10,6 +12,7 @@ import torch
 
 from oracle import draft
 from paper_2410_01228_amd import binding as cs
+import test_asm_hazards
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 DEV = 0x10000                       # stands for device memory: nothing here gets as far as reading it
@@ -240,3 +243,19 @@ def test_struct_is_the_header_s():
     names = re.findall(r"(\w+)(?:\[3\])?;", body)
     assert names == [n for n, _ in cs.cs_rope._fields_]
     assert ctypes.sizeof(cs.cs_rope) == 8 + 4 + 4 + 8 + 8 + 4 + 12 + 8 + 8 + 8
+
+
+@pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"), reason="no hipcc")
+def test_generated_code_around_the_copies_to_lds(tmp_path):
+    """The tree kernels hold the same inline assembly as the prefill kernel: no SCC value lives across it, and none of it reads a matrix result
+    that may not be there."""
+    out = tmp_path / "cs_tree.s"
+    subprocess.run([shutil.which("hipcc") or "/opt/rocm/bin/hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-I" + os.path.join(ROOT, "include"), "-Xclang", "-target-feature",
+                    "-Xclang", "-packed-fp32-ops", "-S", "--cuda-device-only", "-o", str(out), os.path.join(ROOT, "paper_2410_01228_amd", "csrc", "cs_tree.hip")],
+                   check=True, stdout=subprocess.DEVNULL, stderr=subprocess.DEVNULL)
+    text = out.read_text()
+    assert text.count("global_load_lds_dwordx4") > 50 and text.count("v_mfma_f32") > 100
+    assert test_asm_hazards.scc_reads_after_asm(text) == []
+    assert test_asm_hazards.matrix_results_read_in_asm(text) == []
+    # and no kernel keeps what it works with in scratch memory
+    assert set(re.findall(r"\.private_segment_fixed_size: *(\d+)", text)) == {"0"}
