@@ -62,20 +62,32 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
     double least = 0;
     std::vector<float> work, busy;
     for (int64_t trial = whole; trial >= kTreeLeastPiece; trial = trial == whole ? longest : trial * 4 / 5) {
-        work.clear();
-        double partials = 0;
+        // what the launch cannot end before: the slots' share of the work, and the longest piece
+        auto piece_us = [&](const TreeBlocks& t, int32_t keys) { return 8.0 + (keys + 31) / 32 * step_us(t); };
+        double partials = 0, all = 0, longest_us = 0;
+        size_t pieces = 0;
         for (int32_t s = 0; s < S; ++s) {
             const int32_t q = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s], n = b->h_ctx_lens[s] + q, k = pieces_of(s, trial);
             if (k == 0) continue;
             const TreeBlocks t = tree_blocks(q * G);
             const int32_t chunk = tree_chunk_keys(n, k);
-            for (int32_t i = 0; i < k; ++i) {
-                const int32_t keys = std::min(chunk, n - i * chunk);
-                for (int32_t j = 0; j < t.blocks; ++j) work.push_back((float)(8.0 + (keys + 31) / 32 * step_us(t)));
-            }
+            const double full = piece_us(t, chunk), last = piece_us(t, n - (k - 1) * chunk);
+            all += t.blocks * ((k - 1) * full + last);
+            longest_us = std::max(longest_us, full);
+            pieces += (size_t)k * t.blocks;
             if (k > 1) partials += (double)k * t.blocks * t.tiles;
         }
-        if ((int64_t)work.size() > kTreeModelled && trial != whole) break;    // (pieces enough for an even end)
+        if ((int64_t)pieces > kTreeModelled && trial != whole) break;         // (pieces enough for an even end)
+        const double merges = partials > 0 ? 4.0 + partials * Hkv * 16 * D * 8 / 5e6 : 0;
+        if (trial != whole && std::max(all / slots, longest_us) + merges >= least) continue;
+        work.clear();
+        for (int32_t s = 0; s < S; ++s) {
+            const int32_t q = b->h_cu_q_lens[s + 1] - b->h_cu_q_lens[s], n = b->h_ctx_lens[s] + q, k = pieces_of(s, trial);
+            if (k == 0) continue;
+            const TreeBlocks t = tree_blocks(q * G);
+            const int32_t chunk = tree_chunk_keys(n, k);
+            for (int32_t i = 0; i < k; ++i) work.insert(work.end(), t.blocks, (float)piece_us(t, std::min(chunk, n - i * chunk)));
+        }
         std::sort(work.begin(), work.end(), std::greater<float>());
         busy.assign(slots, 0.f);                                 // a heap of when the slots come free
         for (float w : work) {
@@ -83,8 +95,7 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
             busy.back() += w;
             std::push_heap(busy.begin(), busy.end(), std::greater<float>());
         }
-        double end = *std::max_element(busy.begin(), busy.end());
-        if (partials > 0) end += 4.0 + partials * Hkv * 16 * D * 8 / 5e6;
+        const double end = *std::max_element(busy.begin(), busy.end()) + merges;
         if (trial == whole || end < least) { least = end; split = trial; }
     }
     struct Seq { int32_t seq, pieces, blocks, keys; };
@@ -111,7 +122,7 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
 }
 
 // The last plans that the thread made (the workspace query and the calls of the next layers ask for the same one: 64 sequences
-// cost the host 8 us to plan), keyed by everything a plan depends on, the lengths value by value.
+// cost the host 35 us to plan, 256 of them 150; 115 and 540 where every cut was played), keyed by everything a plan depends on, the lengths value by value.
 struct TreeMemo {
     int32_t S = -1, Hq = 0, Hkv = 0, D = 0, cus = 0;
     std::vector<int32_t> ctx, cu;
