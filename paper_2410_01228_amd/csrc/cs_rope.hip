@@ -35,7 +35,7 @@ struct RopeArgs {
     const int32_t* positions;
     int64_t position_stride;
     float eps;
-    int32_t rotary_dim, interleaved, pairs0, pairs1;             // pairs of the first two axes
+    int32_t rotary_dim, interleaved, num_axes, pairs0, pairs1;   // pairs0, pairs1: pairs of the first axis, of the first two
     int32_t T, Hq, Hkv;
     int32_t q_units, kv_units, kv_tokens;                        // wavefronts of a token: with heads of Q; with heads of K, of the tokens in front of kv_tokens
     // the append
@@ -57,10 +57,16 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
+struct __attribute__((packed, aligned(4))) Freqs { float v[4]; };  // (inv_freq is aligned to 4 bytes)
+
 // A thread's features of a row, and the angles of its token.
 struct Turn {
     int32_t off0, off1;                                          // its two pieces of four features
     bool rotates, neighbours;                                    // pairs are (piece 0, piece 1), or neighbours inside a piece
+    // The pieces of all threads lie side by side: rows are read and written 16 bytes a thread (12K tokens of 32/8 heads, rotated in pairs of neighbours, 50.5 us
+    // with 8 bytes, 48 with 16; not rotated 51 and 46.  Heads rotated whole, 16 bytes a thread and the halves changing places between lanes: 49 with
+    // either, and the append 67 us with 8, 71 with 16).
+    bool wide;
     float c[4], s[4];
 };
 
@@ -68,6 +74,7 @@ __device__ __forceinline__ void turn_places(Turn& r, const RopeArgs& a, int32_t 
 {
     r.rotates = 8 * j < a.rotary_dim;
     r.neighbours = a.interleaved != 0 || !r.rotates;
+    r.wide = a.interleaved != 0 || a.rotary_dim == 0;
     r.off0 = r.neighbours ? 8 * j : 4 * j;
     r.off1 = r.neighbours ? 8 * j + 4 : a.rotary_dim / 2 + 4 * j;
 }
@@ -77,18 +84,18 @@ __device__ __forceinline__ void turn_angles(Turn& r, const RopeArgs& a, int32_t 
 #pragma unroll
     for (int i = 0; i < 4; ++i) { r.c[i] = 1.f; r.s[i] = 0.f; }
     if (!r.rotates) return;
-    int32_t at[4];
-    float freq[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int32_t pair = 4 * j + i;
-        at[i] = position;
-        if (a.positions) at[i] = a.positions[(pair < a.pairs0 ? 0 : pair < a.pairs1 ? 1 : 2) * a.position_stride + t];
-        freq[i] = a.inv_freq[pair];
+    // (a load of four frequencies and one of each axis's position; where the token is the wavefront's, those are scalar loads)
+    int32_t axis[3] = {position, position, position};
+    if (a.positions) {
+        axis[0] = axis[1] = axis[2] = a.positions[t];
+        if (a.num_axes > 1) axis[1] = axis[2] = a.positions[a.position_stride + t];
+        if (a.num_axes > 2) axis[2] = a.positions[2 * a.position_stride + t];
     }
+    const Freqs freq = *(const Freqs*)(a.inv_freq + 4 * j);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const double turns = (double)at[i] * (double)freq[i] * 0.15915494309189535;   // 1 / 2 pi
+        const int32_t pair = 4 * j + i, at = pair < a.pairs0 ? axis[0] : pair < a.pairs1 ? axis[1] : axis[2];
+        const double turns = (double)at * (double)freq.v[i] * 0.15915494309189535;   // 1 / 2 pi
         const float part = (float)(turns - rint(turns));
         r.s[i] = __builtin_amdgcn_sinf(part);                    // of a turn: off by 2^-22.9 at most over half a turn (measured at 2^22 points)
         r.c[i] = __builtin_amdgcn_cosf(part);
@@ -164,9 +171,15 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < kRopeRows; ++i) {
             x[i][0] = x[i][1] = r_u32x2{0u, 0u};
-            if (there && h + i * step < end) {
-                x[i][0] = *(const r_u32x2*)(src + (h + i * step) * D + r.off0);
-                x[i][1] = *(const r_u32x2*)(src + (h + i * step) * D + r.off1);
+            if (!there || h + i * step >= end) continue;
+            const uint16_t* row = src + (h + i * step) * D;
+            if (r.wide) {
+                const r_u32x4 v = *(const r_u32x4*)(row + r.off0);
+                x[i][0] = r_u32x2{v[0], v[1]};
+                x[i][1] = r_u32x2{v[2], v[3]};
+            } else {
+                x[i][0] = *(const r_u32x2*)(row + r.off0);
+                x[i][1] = *(const r_u32x2*)(row + r.off1);
             }
         }
     }
@@ -218,6 +231,10 @@ __device__ __forceinline__ void rope_unit(const RopeArgs& a, int32_t unit)
         turn_angles(r, a, j, t, position);
         uint16_t* dst = (is_q ? a.q_out : a.k_out) + (int64_t)t * H * D;
         rows.template finish<E>(r, w, a.eps, h, kAtOnce, H, true, [&](int32_t head, r_u32x2 x0, r_u32x2 x1) {
+            if (r.wide) {
+                __builtin_nontemporal_store(r_u32x4{x0[0], x0[1], x1[0], x1[1]}, (r_u32x4*)(dst + head * D + r.off0));
+                return;
+            }
             __builtin_nontemporal_store(x0, (r_u32x2*)(dst + head * D + r.off0));
             __builtin_nontemporal_store(x1, (r_u32x2*)(dst + head * D + r.off1));
         });
@@ -238,6 +255,10 @@ __device__ __forceinline__ void rope_unit(const RopeArgs& a, int32_t unit)
     rows.template finish<E>(r, w, a.eps, h, kAtOnce, H, true, [&](int32_t head, r_u32x2 x0, r_u32x2 x1) {
         // unit f / 8 of token `slot`, the half of it that the piece is
         uint16_t* blk = page + (int64_t)head * block_elems + slot * 8;
+        if (r.wide) {
+            *(r_u32x4*)(blk + j * a.page_size * 8) = r_u32x4{x0[0], x0[1], x1[0], x1[1]};
+            return;
+        }
         *(r_u32x2*)(blk + (r.off0 >> 3) * a.page_size * 8 + (r.off0 & 7)) = x0;
         *(r_u32x2*)(blk + (r.off1 >> 3) * a.page_size * 8 + (r.off1 & 7)) = x1;
     });
@@ -409,7 +430,7 @@ static int fill_rope(const cs_rope* r, const void* q, int64_t q_stride, const vo
     a.position_stride = r->position_stride;
     a.eps = r->eps;
     a.rotary_dim = r->rotary_dim; a.interleaved = r->interleaved;
-    a.pairs0 = ends[0]; a.pairs1 = ends[1];
+    a.num_axes = r->num_axes; a.pairs0 = ends[0]; a.pairs1 = ends[1];
     a.T = T; a.Hq = Hq; a.Hkv = Hkv;
     return CS_OK;
 }
