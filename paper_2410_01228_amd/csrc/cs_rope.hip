@@ -12,7 +12,7 @@
 // Where rows are written (Q, and K without a cache) a wavefront takes eight heads (16 of head dim 64) of one token, 2 KiB that lie
 // side by side, so that its angles serve two rows of a lane, all of it is one trip to memory, and
 // a launch has wavefronts enough to keep the memory busy (workgroups that walked 16 tokens' heads with the angles computed once ran at
-// half the rate: 10K tokens appended, 32/8 heads, 96 us where this takes 64, at 4.7 TB/s).  Where K and V go to a page a workgroup takes its 16 tokens and a few heads.
+// half the rate: 12K tokens appended, 32/8 heads, 96 us where this takes 65, at 4.7 TB/s).  Where K and V go to a page a workgroup takes its 16 tokens and a few heads.
 #include <algorithm>
 #include "cs_common.h"
 #include "cs_elem.h"
