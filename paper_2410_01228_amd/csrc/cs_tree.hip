@@ -150,15 +150,17 @@ static const TreePlan& tree_plan_for(const cs_batch* b, int32_t Hq, int32_t Hkv,
 template <int D, class E, int PS>
 static void launch_tree(const TreePlan& p, const cs_kv_pool& pool, const uint16_t* layer_base, const cs_batch& b, int32_t G, const uint64_t* mask, int32_t mask_words,
                         const uint16_t* q, uint16_t* out, float scale_log2e, const TreePartials& part, const TreeItems& items, int32_t n, hipStream_t st) {
-    const dim3 grid((uint32_t)n * (uint32_t)pool.num_kv_heads);
-#define CS_LAUNCH_TREE(KERNEL, NC)                                                                                                   \
+    const int32_t spread = p.tiles > 2 ? tree_spread_items(n, pool.num_kv_heads) : 0;
+    const dim3 grid((uint32_t)(spread > 0 ? spread : n) * (uint32_t)pool.num_kv_heads);
+#define CS_LAUNCH_TREE(KERNEL, NC, ...)                                                                                              \
     hipLaunchKernelGGL((KERNEL<D, E, PS, NC>), grid, dim3(kDecodeThreads), 0, st, layer_base, pool.page_stride, pool.num_pages,        \
-                       pool.num_kv_heads, G, b.block_tables, b.max_blocks_per_seq, b.ctx_lens, b.cu_q_lens, mask, mask_words, q, out, scale_log2e, part, items)
-    if (p.tiles == 1) CS_LAUNCH_TREE(tree_kernel, 1);
-    else if (p.tiles == 2) CS_LAUNCH_TREE(tree_kernel, 2);
-    else if (p.tiles == 4) CS_LAUNCH_TREE(tree_ring_kernel, 1);
-    else if (p.tiles == 8) CS_LAUNCH_TREE(tree_ring_kernel, 2);
-    else CS_LAUNCH_TREE(tree_ring_kernel, 3);
+                       pool.num_kv_heads, G, b.block_tables, b.max_blocks_per_seq, b.ctx_lens, b.cu_q_lens, mask, mask_words, q, out, scale_log2e, part, __VA_ARGS__)
+    const int32_t n_spread = spread > 0 ? n : 0;
+    if (p.tiles == 1) CS_LAUNCH_TREE(tree_kernel, 1, items);
+    else if (p.tiles == 2) CS_LAUNCH_TREE(tree_kernel, 2, items);
+    else if (p.tiles == 4) CS_LAUNCH_TREE(tree_ring_kernel, 1, n_spread, items);
+    else if (p.tiles == 8) CS_LAUNCH_TREE(tree_ring_kernel, 2, n_spread, items);
+    else CS_LAUNCH_TREE(tree_ring_kernel, 3, n_spread, items);
 #undef CS_LAUNCH_TREE
 }
 

@@ -426,11 +426,17 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
     const uint16_t* __restrict__ layer_base, int64_t page_stride, int32_t num_pages, int32_t Hkv, int32_t G,
     const int32_t* __restrict__ block_tables, int32_t max_blocks, const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ cu_q_lens,
     const uint64_t* __restrict__ mask, int32_t mask_words, const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
-    float scale_log2e, TreePartials part, const TreeItems items)
+    float scale_log2e, TreePartials part, const int32_t n_spread, const TreeItems items)
 {
     typedef RingLds<D, NC> Lds;
     __shared__ Lds lds;
-    const int32_t item = (int32_t)blockIdx.x / Hkv, g = (int32_t)blockIdx.x - item * Hkv;
+    int32_t item = (int32_t)blockIdx.x / Hkv, g = (int32_t)blockIdx.x - item * Hkv;
+    if (n_spread > 0) {                                          // (see tree_spread_items)
+        const int32_t sets = 8 / Hkv, turn = (int32_t)(blockIdx.x >> 3), set = (int32_t)(blockIdx.x & 7) / Hkv;
+        g = (int32_t)(blockIdx.x & 7) - set * Hkv;
+        item = (turn / kTreeRun * sets + set) * kTreeRun + turn % kTreeRun;
+        if (item >= n_spread) return;
+    }
     const TreeItem it = tree_item(items.e[item]);
     const int32_t s = it.seq, t0 = cu_q_lens[s], q_len = cu_q_lens[s + 1] - t0, ctx = ctx_lens[s];
     const int32_t n_keys = ctx + q_len, rows = q_len * G;
