@@ -45,7 +45,7 @@ struct TreeItems {
 };
 
 // Workgroups go round the eight XCDs.  Of fewer than eight kv heads the blocks of a piece would land on several, each of which fetches the same K and V: with
-// 4 kv heads (28/4, 16 trees of 24-64 nodes on 1000-8192 keys: 333 MB fetched for 175) the items are dealt to 8 / Hkv sets of XCDs, kTreeRun neighbours in turn,
+// 4 kv heads (28/4, 16 trees of 24-64 nodes on 1000-8192 keys: 333 MB fetched for 175, 198 if dealt as follows) the items are dealt to 8 / Hkv sets of XCDs, kTreeRun neighbours in turn,
 // and launched in whole rounds of that.  (119 us as they come, 118 one by one, 113 by twos, 110 by fours, 114 by eights; 32 such trees 158, 157, 154, 152, 150.)
 constexpr int kTreeRun = 4;
 inline int32_t tree_spread_items(int32_t items, int32_t Hkv) {   // as many as are launched; 0: they go as they come
