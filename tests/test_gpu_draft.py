@@ -368,6 +368,18 @@ def test_every_number_of_row_tiles(D, page_size, dtype):
         check_tree(w, q, G, masks, D ** -0.5, run_tree(w, q, G, masks, D ** -0.5))
 
 
+@pytest.mark.parametrize("S", [1, 2, 5, 9, 17])
+@pytest.mark.parametrize("Hkv", [1, 2, 3, 4, 6])
+def test_blocks_of_few_kv_heads(Hkv, S):
+    """Work items are dealt to the XCDs in whole rounds where the kv heads divide their number: counts that fill no round, blocks and pieces among them."""
+    G, D, rng = 4, 64, np.random.default_rng(100 * Hkv + S)
+    new = rng.integers(17, 130, S).tolist()
+    w = World(rng.integers(0, 1500, S).tolist(), new, Hkv, D, 10 * Hkv + S)
+    q = tree_step(w, Hkv * G, w.rng)
+    masks = [draft.ancestors(random_tree(w.rng, n, 5)) for n in new]
+    check_tree(w, q, Hkv * G, masks, D ** -0.5, run_tree(w, q, Hkv * G, masks, D ** -0.5))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("page_size", [16, 8])
 @pytest.mark.parametrize("D", [64, 128])
