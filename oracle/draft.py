@@ -79,9 +79,9 @@ def ref_verify(tokens, parents, p, q, u, u_next):
     at, path = 0, [0]
     clean = lambda x: np.where(np.isnan(x), 0.0, np.maximum(x, 0.0))  # noqa: E731
     while True:
-        row = np.asarray(p[at], np.float64)
-        draft = None if q is None else np.asarray(q[at], np.float64)
-        left, z, c, went = clean(row), 1.0, 0.0, None
+        row = clean(np.asarray(p[at], np.float64))
+        draft = None if q is None else clean(np.asarray(q[at], np.float64))
+        left, z, c, went = row.copy(), 1.0, 0.0, None
         for j in range(at + 1, n):
             if parents[j] != at:
                 continue
@@ -105,7 +105,7 @@ def ref_verify(tokens, parents, p, q, u, u_next):
         at = went
         path.append(at)
     if not (left > 0).any():
-        left = clean(row)
+        left = row
     run = np.cumsum(left)
     hit = np.nonzero((run > float(u_next) * run[-1]) & (left > 0))[0]
     some = np.nonzero(left > 0)[0]

@@ -87,11 +87,13 @@ __device__ __forceinline__ void load_nodes(const VerifyArgs& a, int32_t t0, Node
     }
 }
 
-// What is left of an element.
+// What is left of an element.  One that is negative or no number counts as nothing: of p the last maximum sees to it, since c and what counts of q are
+// not negative; q has one of its own.  (After the conversion: the maximum of a loaded float takes two instructions, the first for signalling
+// NaN.  16 drawn trees of 32, 128256 probabilities: 44.4 us with those for both, 40.0 so, 38.8 without any.)
 template <bool kDrawn>
 __device__ __forceinline__ double left_of(float p, float q, double c) {
     if (!kDrawn) return fmax((double)p, 0.0);
-    return fmax((double)p - c * (double)q, 0.0);                 // (not a number counts as nothing)
+    return fmax((double)p - c * fmax((double)q, 0.0), 0.0);
 }
 
 // Goes on from (node, last) until no child is left or the sum of a row is needed.  z: the weight of what is left, negative: not known.
@@ -124,7 +126,7 @@ __device__ __forceinline__ void walk(const Nodes& d, VerifyLds& s, int32_t node,
                 again = again || __any(d.parent[k] == node && d.token[k] == token && k * 64 + lane < child);
             if (again) r = 0.0;
         }
-        const double bar = kDrawn ? (double)u * (double)q * z : (double)u * z;
+        const double bar = kDrawn ? (double)u * fmax((double)q, 0.0) * z : (double)u * z;
         if (bar < r) {
             if (lane == 0) s.path[len] = child;
             ++len;

@@ -814,3 +814,36 @@ def test_the_same_bits_every_time():
     for _ in range(20):
         step()
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("vocab", [6, 40, 3000, 50257])
+def test_verification_takes_malformed_elements_of_either_row_as_nothing(vocab):
+    """Negative elements, infinities below zero and NaN (signalling ones among them), in p and in q, at drafted tokens and elsewhere: as if they were 0."""
+    d = Drafts([9] * (40 if vocab < 5000 else 6), vocab, True, 90 + vocab, width=2, sharp=1.0)
+    clean = []
+    for x in (d.p, d.q):
+        kind, at = d.rng.integers(0, 6, x.shape), d.rng.random(x.shape) < 0.3
+        for s, n in enumerate(d.new):                             # half of the drafts' own elements
+            for i in range(1, n):
+                t = d.cu[s] + i
+                at[d.cu[s] + d.parents[t], d.tokens[t]] = d.rng.random() < 0.5
+        for k, bad in enumerate((np.float32(-0.0), np.float32(-np.inf), np.float32(np.nan), np.uint32(0x7FA00001).view(np.float32))):
+            x.view(np.uint32)[at & (kind == k)] = np.asarray(bad).view(np.uint32)
+        x[at & (kind > 3)] *= -2
+        clean.append(np.where(at, np.float32(0), x))
+    args = d.device()
+    cs.cs_spec_verify(*args)
+    lens = d.check(args)                                          # as the header has it
+    d.p, d.q = clean
+    assert lens == d.check(args) and sum(lens) > len(lens)           # and as rows that hold zeros there
+
+
+def test_a_draft_that_the_target_never_has_is_refused_however_negative_q_is():
+    d = Drafts([3] * 8, 20, True, 91)
+    d.p[:], d.q[:] = 0.0, 1.0 / 20
+    d.p[:, 7] = 1.0
+    d.tokens[:], d.parents[:] = 3, np.tile([-1, 0, 1], 8)
+    d.q[::3, 3] = [-1.0, -0.25, -1e-30, -np.inf, -3e38, -0.0, np.nan, 0.25]
+    args = d.device()
+    cs.cs_spec_verify(*args)
+    assert args[9][:8].tolist() == [1] * 8 and args[7][:24:3].tolist() == [7] * 8
