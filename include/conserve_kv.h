@@ -559,7 +559,7 @@ int cs_paged_attention_tree_f16(const cs_kv_pool* pool, int32_t layer, const cs_
  * and the walk goes on from it; where no child is accepted, or there is none, the token that follows is the first one at which the running sum of
  * R passes u_next[s] * sum R.  With u, u_next uniform on [0, 1) the tokens are distributed as p's own.  All decisions in
  * fp64.  Where nothing is left of R it is p[n] that is drawn from; where there is nothing either, the token is -1.  An element of p or q that
- * is negative or no number counts as 0; a token outside the vocabulary is refused.
+ * is negative or no number counts as 0; a token of which nothing is left, or outside the vocabulary, is refused, whatever u is.
  *   tokens, parents, u: device [T], entries of node 0 not read; parents[i] < i, in the sequence's own numbers (a node whose parent
  *   is none of 0 .. i - 1 is never reached), NULL: a chain.  p, q: device fp32, the row of token t from p + t * p_stride on
  *   (strides in elements, >= vocab); the distribution behind t, and the one that t's children were drawn from (not read where

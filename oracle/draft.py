@@ -89,7 +89,7 @@ def ref_verify(tokens, parents, p, q, u, u_next):
             inside = 0 <= x < vocab
             r = left[x] if inside else 0.0
             bar = float(u[j]) * z if draft is None else float(u[j]) * (draft[x] if inside else 0.0) * z
-            if bar < r:
+            if bar < r and r > 0:
                 went = j
                 break
             if draft is None:

@@ -127,7 +127,7 @@ __device__ __forceinline__ void walk(const Nodes& d, VerifyLds& s, int32_t node,
             if (again) r = 0.0;
         }
         const double bar = kDrawn ? (double)u * fmax((double)q, 0.0) * z : (double)u * z;
-        if (bar < r) {
+        if (bar < r && r > 0.0) {                                // (a bar below zero passes no token of which nothing is left)
             if (lane == 0) s.path[len] = child;
             ++len;
             node = last = child;

@@ -847,3 +847,29 @@ def test_a_draft_that_the_target_never_has_is_refused_however_negative_q_is():
     args = d.device()
     cs.cs_spec_verify(*args)
     assert args[9][:8].tolist() == [1] * 8 and args[7][:24:3].tolist() == [7] * 8
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_what_has_no_probability_is_refused_whatever_the_random_number_is(drawn):
+    """Random numbers below 0, and guesses whose refusals take more than 1 from a row: the bar is negative, and nothing is left of the token."""
+    vocab, outside = 9, [-1, 9, 2 ** 31 - 1, -2 ** 31]
+    d = Drafts([2] * 5 + [4] * 4, vocab, drawn, 92)
+    d.p[:], d.q[:] = 0.0, 1.0 / vocab
+    d.p[:, 2] = 1.0
+    d.u[:] = -1.0
+    for s in range(5):
+        d.tokens[2 * s + 1] = outside[s] if s < 4 else 5          # 5: inside, but the target never has it
+        d.parents[2 * s:2 * s + 2] = [-1, 0]
+    for s in range(4):                                            # children 2 and 4 have 0.75 each of a row, the third one nothing
+        t = 10 + 4 * s
+        d.p[t] = 0.0
+        d.p[t, [2, 4]] = 0.75
+        d.tokens[t:t + 4] = [0, 2, 4, outside[s]]
+        d.parents[t:t + 4] = [-1, 0, 0, 0]
+        d.u[t:t + 4] = 20.0
+    d.u_next[:] = 0.0
+    args = d.device()
+    cs.cs_spec_verify(*args)
+    assert args[9][:9].tolist() == [1] * 9
+    assert args[7][:10:2].tolist() == [2] * 5 and args[7][10:26:4].tolist() == [2] * 4
+    d.check(args)
