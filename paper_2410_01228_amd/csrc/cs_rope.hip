@@ -273,13 +273,22 @@ __device__ __forceinline__ void rope_unit(const RopeArgs& a, int32_t unit)
     }
 }
 
+// LDS of a workgroup that fills a page: rows of K and V, read and written 16 bytes at a time.
+template <int D>
+struct SlotLds {
+    static constexpr int kHeads = kRopeThreads / (D / 8 * kRopeTokens);              // heads at once
+    alignas(16) uint16_t k[kRopeRows][kHeads][kRopeTokens][D + 8];
+    alignas(16) uint16_t v[kRopeRows][kHeads][kRopeTokens][D + 8];
+};
+
 // K and V of the 16 positions of a slot, heads kv0 .. of one part; kRopeRows * kHeads heads a round.
 template <int D, class E>
 __device__ __forceinline__ void rope_slot(const RopeArgs& a, int32_t block)
 {
     constexpr int kLanes = D / 8;                                // threads of a row
-    constexpr int kHeads = kRopeThreads / (kLanes * kRopeTokens);// heads at once
-    __shared__ uint16_t k_tile[kRopeRows][kHeads][kRopeTokens][D + 8], v_tile[kRopeRows][kHeads][kRopeTokens][D + 8];
+    constexpr int kHeads = SlotLds<D>::kHeads;
+    __shared__ SlotLds<D> lds;
+    auto &k_tile = lds.k, &v_tile = lds.v;
     const int32_t tid = threadIdx.x, j = tid % kLanes, tok = tid / kLanes % kRopeTokens, sub = tid / (kLanes * kRopeTokens);
     const int32_t slot_id = block / a.slot_groups, part = block - slot_id * a.slot_groups;
     const int32_t kv0 = (int32_t)((int64_t)part * a.Hkv / a.slot_groups), kv1 = (int32_t)((int64_t)(part + 1) * a.Hkv / a.slot_groups);

@@ -28,7 +28,7 @@ template <int D, int NC>
 struct TreeLds {
     u32x4 q[NC][D / 32][64];                                // Q as the B operand, lane by lane
     uint64_t mask[16 * NC + 1][kTreeWords + 1];                  // masks of the block's nodes, a word of zeros behind each
-    float o[kDecodeWaves][16][D + 4];                            // one tile's partial outputs of the wavefronts
+    alignas(16) float o[kDecodeWaves][16][D + 4];                // one tile's partial outputs of the wavefronts, four floats at a time
     float m[kDecodeWaves][NC][16], l[kDecodeWaves][NC][16];
     int32_t odd;                                                 // a step met a V that is not finite
 };
@@ -417,7 +417,7 @@ constexpr int kTreeRing = 4;
 template <int D, int NC>
 struct RingLds {
     static constexpr int kBlock = 16 * D * 2, kSlot = 4 * kBlock + 64;               // bytes
-    char ring[kTreeRing][kSlot];
+    alignas(16) char ring[kTreeRing][kSlot];
     uint64_t mask[16 * 4 * NC + 1][kTreeWords + 1];
 };
 

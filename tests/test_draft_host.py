@@ -259,3 +259,21 @@ def test_generated_code_around_the_copies_to_lds(tmp_path):
     assert test_asm_hazards.matrix_results_read_in_asm(text) == []
     # and no kernel keeps what it works with in scratch memory
     assert set(re.findall(r"\.private_segment_fixed_size: *(\d+)", text)) == {"0"}
+
+
+@pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"), reason="no hipcc")
+def test_what_lds_is_read_by_sixteen_bytes_is_aligned_to_them(tmp_path):
+    """Members of the kernels' LDS that they access as vectors of 16 bytes: their places, their rows and the blocks themselves."""
+    csrc = os.path.join(ROOT, "paper_2410_01228_amd", "csrc")
+    lines = ['#include "cs_tree_impl.h"', '#include "cs_rope.hip"', "using namespace cs;"]
+    for d in (64, 128):
+        kinds = [("TreeLds<%d, %d>" % (d, nc), ("q", "o"), ("o[0][0]",)) for nc in (1, 2)] + [("RingLds<%d, %d>" % (d, nc), ("ring",), ("ring[0]",)) for nc in (1, 2, 3)]
+        for kind, members, rows in kinds + [("SlotLds<%d>" % d, ("k", "v"), ("k[0][0][0]", "v[0][0][0]"))]:
+            lines.append("{ typedef %s T; static_assert(alignof(T) %% 16 == 0);" % kind)
+            lines += ["static_assert(__builtin_offsetof(T, %s) %% 16 == 0);" % m for m in members]
+            lines += ["static_assert(sizeof(((T*)nullptr)->%s) %% 16 == 0);" % r for r in rows] + ["}"]
+    source = tmp_path / "places.hip"
+    source.write_text("\n".join(lines[:3]) + "\nvoid places() {\n" + "\n".join(lines[3:]) + "\n}\n")
+    run = subprocess.run([shutil.which("hipcc") or "/opt/rocm/bin/hipcc", "--offload-arch=gfx950", "-std=c++17", "-fsyntax-only", "--cuda-host-only", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                          str(source)], capture_output=True, text=True)
+    assert run.returncode == 0, run.stderr
