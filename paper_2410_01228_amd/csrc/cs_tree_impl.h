@@ -19,6 +19,9 @@ namespace cs {
 
 constexpr int kTreeKeys = 32;                                    // keys of a step
 constexpr float kTreeSlack = 6.f;                                // a running maximum may lie this far (in powers of two) below the scores
+// What a running maximum starts from: no score is less, and a score of -infinity (masked, or K or Q are infinite or their product is) is
+// infinitely far below it, so that its weight is 0.  (From -infinity on it would be no number until a finite score came.)
+constexpr float kTreeLeast = -3.402823466e38f;
 
 // Wavefronts of a SIMD: outputs of NC tiles (D / 4 registers each), two steps of K and V (D / 2 each) and the rest.
 constexpr int tree_waves(int D, int NC) { return D * NC >= 256 ? 1 : 2; }
@@ -119,27 +122,26 @@ __device__ __forceinline__ void tree_scores(const TreeKv<D>& r, const u32x4 (*q)
     for (int i = 0; i < 4; ++i) { x[i] = sa[i]; x[4 + i] = sb[i]; }
 }
 
-// The scores' weights, rounded to the element type: an operand of the product with V.  kTail: some scores may be -infinity (not seen).
-template <int D, class E, int NC, bool kTail>
+// The scores' weights, rounded to the element type: an operand of the product with V.  A score of -infinity (not seen, or so far off) weighs 0.
+template <int D, class E, int NC>
 __device__ __forceinline__ u32x4 tree_weights(TreeState<D, NC>& st, int c, const float (&x)[8], float scale_log2e)
 {
     // The maximum moves only when a score lies 2^6 above it, and only then do the lanes of a row look at each other's scores.
     const float mine = max8(x);
-    if (__any(__builtin_fmaf(mine, scale_log2e, -st.m[c]) > kTreeSlack)) {       // (nothing seen before: the maximum is -infinity)
+    if (__any(__builtin_fmaf(mine, scale_log2e, -st.m[c]) > kTreeSlack)) {
         float mx = mine * scale_log2e;
         mx = xor_max(mx, 16);
         mx = xor_max(mx, 32);
-        const float m_new = fmaxf(st.m[c], mx), mu = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = exp2f(st.m[c] - mu);                 // 0 where nothing was seen before
+        const float m_new = fmaxf(st.m[c], mx);
+        const float alpha = exp2f(st.m[c] - m_new);              // 0 where nothing was seen before
         st.l[c] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[c][dt] *= alpha;
         st.m[c] = m_new;
     }
-    const float mu = kTail && st.m[c] == -INFINITY ? 0.f : st.m[c];
     float p[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale_log2e, -mu));
+    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale_log2e, -st.m[c]));
     const u32x4 pb = { E::pack(p[0], p[1]), E::pack(p[2], p[3]), E::pack(p[4], p[5]), E::pack(p[6], p[7]) };
     st.l[c] = sum_weights<E>(p, pb, st.l[c]);
     return pb;
@@ -167,7 +169,7 @@ __device__ __forceinline__ void tree_step(TreeState<D, NC>& st, const TreeKv<D>&
 #pragma unroll
     for (int c = 0; c < T; ++c) {
         if (c + 1 < T) tree_scores<D, E>(r, q[c + 1], lane, x[(c + 1) & 1]);
-        const u32x4 pb = tree_weights<D, E, NC, false>(st, c, x[c & 1], scale_log2e);
+        const u32x4 pb = tree_weights<D, E, NC>(st, c, x[c & 1], scale_log2e);
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[c][dt] = E::mfma32(r.both(dt), pb, st.o[c][dt]);
     }
@@ -214,7 +216,7 @@ __device__ __forceinline__ void tree_tail_step(TreeState<D, NC>& st, TreeKv<D>& 
             x[i] = w >> i & 1u ? x[i] : -INFINITY;
             x[4 + i] = w >> (16 + i) & 1u ? x[4 + i] : -INFINITY;
         }
-        const u32x4 pb = tree_weights<D, E, NC, true>(st, c, x, scale_log2e);
+        const u32x4 pb = tree_weights<D, E, NC>(st, c, x, scale_log2e);
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[c][dt] = E::mfma32(r.both(dt), pb, st.o[c][dt]);
     }
@@ -324,7 +326,7 @@ __global__ __launch_bounds__(kDecodeThreads, (tree_waves(D, NC))) void tree_kern
     TreeState<D, NC> st;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        st.m[c] = -INFINITY;
+        st.m[c] = kTreeLeast;
         st.l[c] = 0.f;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[c][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -381,8 +383,7 @@ __global__ __launch_bounds__(kDecodeThreads, (tree_waves(D, NC))) void tree_kern
 #pragma unroll
             for (int w = 0; w < kDecodeWaves; ++w) {
                 const float mw = lds.m[w][c][i], lw = lds.l[w][c][i];
-                if (mw == -INFINITY && lw == 0.f) continue;      // (not a weight of zero: an infinity in V stays one)
-                const float f = exp2f(mw - M);
+                const float f = exp2f(mw - M);                   // (a wavefront that saw nothing has nothing to weigh)
                 L += lw * f;
                 O += *(const f32x4*)&lds.o[w][i][d] * f;
             }
@@ -519,7 +520,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
             qb[c][kk] = u32x4{0u, 0u, 0u, 0u};
             if (c < tiles && row < rows) qb[c][kk] = *(const u32x4*)(q + ((int64_t)(t0 + node) * Hq + g * G + head) * D + kk * 32 + (lane >> 4) * 8);
         }
-        st.m[c] = -INFINITY;
+        st.m[c] = kTreeLeast;
         st.l[c] = 0.f;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[c][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -577,7 +578,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
             for (int c = 0; c < T; ++c) scores(slot, c, x[c]);
             ahead(i);                                            // (behind the first reads of this step)
 #pragma unroll
-            for (int c = 0; c < T; ++c) pb[c] = tree_weights<D, E, NC, false>(st, c, x[c], scale_log2e);
+            for (int c = 0; c < T; ++c) pb[c] = tree_weights<D, E, NC>(st, c, x[c], scale_log2e);
             if constexpr (T > 0) {
 #pragma unroll
                 for (int dt = 0; dt < D / 16; ++dt) {
@@ -608,7 +609,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
             const uint32_t w = seen_window(lds.mask[node], key0 - ctx, valid);
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = w >> j & 1u ? x[j] : -INFINITY;
-            pb[c] = tree_weights<D, E, NC, true>(st, c, x, scale_log2e);
+            pb[c] = tree_weights<D, E, NC>(st, c, x, scale_log2e);
         }
         // slots behind the last token hold whatever was there; infinities and NaN: see tree_tail_step
 #pragma unroll
@@ -669,7 +670,7 @@ __global__ __launch_bounds__(4 * D) void tree_merge_kernel(
     if (c >= blocks.tiles) return;
     const int32_t r = (int32_t)threadIdx.x / (D / 4), d = ((int32_t)threadIdx.x - r * (D / 4)) * 4, row = (it.block * blocks.tiles + c) * 16 + r;
     if (row >= rows) return;
-    float M = -INFINITY, L = 0.f;
+    float M = kTreeLeast, L = 0.f;
     f32x4 O = {0.f, 0.f, 0.f, 0.f};
     const int64_t at = ((int64_t)merges.e[merge].item * Hkv + g) * part_rows + c * 16 + r, next = (int64_t)blocks.blocks * Hkv * part_rows;
     // eight pieces' loads in flight at once; with more of them the maxima are read twice
@@ -696,7 +697,7 @@ __global__ __launch_bounds__(4 * D) void tree_merge_kernel(
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (i0 + i >= it.pieces || (ml[i][0] == -INFINITY && ml[i][1] == 0.f)) continue;     // (not a weight of zero: an infinity in V stays one)
+            if (i0 + i >= it.pieces) continue;
             const float f = exp2f(ml[i][0] - M);
             L += ml[i][1] * f;
             O += o[i] * f;

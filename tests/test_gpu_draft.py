@@ -873,3 +873,44 @@ def test_what_has_no_probability_is_refused_whatever_the_random_number_is(drawn)
     assert args[9][:9].tolist() == [1] * 9
     assert args[7][:10:2].tolist() == [2] * 5 and args[7][10:26:4].tolist() == [2] * 4
     d.check(args)
+
+
+def infinitely_far(w, s, first, end, value):
+    """K of the keys first .. end - 1 of sequence s gets `value` as its first feature, in every head: all of their scores are -infinity for queries
+    with a positive one there."""
+    for key in range(first, end):
+        w.pool[w.layer, w.tables[s, key // w.ps], 0, :, kv_layout.k_index(key % w.ps, 0, w.D, page_size=w.ps)] = value
+
+
+def near_without(w, q, Hq, masks, scale, got, first, end):
+    """The keys first .. end - 1 of each sequence's cached ones weigh nothing: exp(-infinity - m) for a finite m."""
+    for s in range(len(w.ctx)):
+        n, t0 = w.new[s], int(w.cu[s])
+        k, v = (np.concatenate([x[:first[s]], x[end[s]:]]) for x in w.logical(s))
+        seen = np.tril(np.ones((n, n), bool)) if masks is None else masks[s][:, :n]
+        want, tol = draft.ref_tree_attention(q[t0:t0 + n].double().numpy(), k, v, seen, scale, HALF_STEP[w.dtype], w.dtype == F16)
+        near(got[t0:t0 + n].double().numpy(), want, tol, (s, w.ctx[s], n))
+
+
+# -infinity, and for bf16 a finite one whose products with q are below the least float
+NEGATIVE = [(BF16, 0xFF80), (F16, 0xFC00), (BF16, 0xFF7F)]
+
+
+@pytest.mark.parametrize("dtype,value", NEGATIVE)
+@pytest.mark.parametrize("page_size", [16, 8])
+@pytest.mark.parametrize("Hq,Hkv,D,ctx,new,first,end", [
+    (4, 2, 64, (400, 300), (4, 2), (0, 0), (200, 160)),           # wavefronts that share the keys, whose first steps hold nothing else
+    (16, 2, 128, (400, 300), (3, 1), (0, 40), (200, 290)),
+    (8, 2, 64, (400, 90), (40, 9), (0, 3), (200, 90)),            # that share the rows
+    (16, 2, 128, (300, 0), (60, 5), (0, 0), (300, 0)),            # one to three tiles each; nodes see nothing else but nodes
+    (4, 2, 128, (9000, 3), (4, 1), (0, 0), (6000, 3)),            # whole pieces of a cut sequence
+    (32, 2, 64, (9000,), (30,), (100,), (8990,)),
+])
+def test_keys_infinitely_far_weigh_nothing(Hq, Hkv, D, ctx, new, first, end, page_size, dtype, value):
+    w = World(ctx, new, Hkv, D, 93, dtype, page_size)
+    q = tree_step(w, Hq, w.rng)
+    q[..., 0] = q[..., 0].abs() + 1.5
+    for s in range(len(ctx)):
+        infinitely_far(w, s, first[s], end[s], value)
+    masks = [draft.ancestors(random_tree(w.rng, n, 4)) for n in new]
+    near_without(w, q, Hq, masks, 2.0, run_tree(w, q, Hq, masks, 2.0), first, end)
