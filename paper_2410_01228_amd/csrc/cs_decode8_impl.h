@@ -85,9 +85,9 @@ __device__ __forceinline__ void process_step8(WaveState<D>& st, const StepRegs8<
     float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     mx = xor_max(mx, 16);
     mx = xor_max(mx, 32);
-    const float m_new = fmaxf(st.m, mx);               // finite: token tok0 is always valid
+    const float m_new = fmaxf(st.m, mx);               // (no score is less than the least float)
     if (__any(m_new > st.m)) {
-        const float alpha = exp2f(st.m - m_new);       // 0 on the first step (m = -inf)
+        const float alpha = exp2f(st.m - m_new);       // 0 on the first step
         st.l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[dt] *= alpha;
@@ -183,7 +183,7 @@ __device__ __forceinline__ void decode_item8(
     }
 
     WaveState<D> st;
-    st.m = -INFINITY;
+    st.m = kLeastMax;
     st.l = 0.f;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) st.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};

@@ -119,6 +119,10 @@ __device__ __forceinline__ void load_page(PageRegs<D>& r, const uint16_t* __rest
         r.v[dt] = __builtin_nontemporal_load((const u32x2*)vblk + dt * 32 + voff);
 }
 
+// What a running maximum starts from: no score is less, and one of -infinity (masked, or K or Q are infinite or their product is) is infinitely far below
+// it, so that it weighs 0.  (From -infinity on it would be no number until a finite score came.)
+constexpr float kLeastMax = -3.402823466e38f;
+
 // One wavefront's running state.
 template <int D>
 struct WaveState {
@@ -146,9 +150,9 @@ __device__ __forceinline__ void process_page(WaveState<D>& st, const PageRegs<D>
     float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
     mx = xor_max(mx, 16);
     mx = xor_max(mx, 32);
-    const float m_new = fmaxf(st.m, mx);               // finite: token tok0 is always valid
+    const float m_new = fmaxf(st.m, mx);               // (no score is less than the least float)
     if (__any(m_new > st.m)) {
-        const float alpha = exp2f(st.m - m_new);       // 0 on the first page (m = -inf)
+        const float alpha = exp2f(st.m - m_new);       // 0 on the first page
         st.l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[dt] *= alpha;
@@ -257,7 +261,7 @@ __device__ __forceinline__ void merge_pieces(const DecodePartials& part, int32_t
     const Shared pm(part.ml + row0 * 2, (uint32_t)n_splits * Hq * 8);
     for (int idx = threadIdx.x; idx < G * kQuads; idx += kDecodeThreads) {
         const int head = idx / kQuads, quad = idx - head * kQuads;
-        float M = -INFINITY, L = 0.f;
+        float M = kLeastMax, L = 0.f;
         f32x4 O = {0.f, 0.f, 0.f, 0.f};
         for (int32_t i0 = 0; n_splits > 8 && i0 < n_splits; i0 += 8) {
             a_u32x2 ml[8];
@@ -283,7 +287,7 @@ __device__ __forceinline__ void merge_pieces(const DecodePartials& part, int32_t
             for (int j = 0; j < 8; ++j) {
                 if (i0 + j >= n_splits) break;                             // (not a weight of zero: an infinity in V stays one)
                 const float m = as_float(ml[j][0]);
-                const float f = m == -INFINITY ? 0.f : exp2f(m - M);                              // a piece without keys
+                const float f = exp2f(m - M);                              // (a piece without keys has nothing to weigh)
                 L += as_float(ml[j][1]) * f;
                 O += __builtin_bit_cast(f32x4, o[j]) * f;
             }
@@ -329,7 +333,7 @@ __device__ __forceinline__ void leave_item(
 #pragma unroll
         for (int w = 0; w < kDecodeWaves; ++w) {
             const float mw = sh_m[w][head];
-            const float f = mw == -INFINITY ? 0.f : exp2f(mw - M);     // a wavefront without pages
+            const float f = exp2f(mw - M);                             // (a wavefront without pages has nothing to weigh)
             L += sh_l[w][head] * f;
             O += sh_o[w][head][d] * f;
         }
@@ -419,7 +423,7 @@ __device__ __forceinline__ void decode_item(
     }
 
     WaveState<D> st;
-    st.m = -INFINITY;
+    st.m = kLeastMax;
     st.l = 0.f;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) st.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};

@@ -19,9 +19,6 @@ namespace cs {
 
 constexpr int kTreeKeys = 32;                                    // keys of a step
 constexpr float kTreeSlack = 6.f;                                // a running maximum may lie this far (in powers of two) below the scores
-// What a running maximum starts from: no score is less, and a score of -infinity (masked, or K or Q are infinite or their product is) is
-// infinitely far below it, so that its weight is 0.  (From -infinity on it would be no number until a finite score came.)
-constexpr float kTreeLeast = -3.402823466e38f;
 
 // Wavefronts of a SIMD: outputs of NC tiles (D / 4 registers each), two steps of K and V (D / 2 each) and the rest.
 constexpr int tree_waves(int D, int NC) { return D * NC >= 256 ? 1 : 2; }
@@ -326,7 +323,7 @@ __global__ __launch_bounds__(kDecodeThreads, (tree_waves(D, NC))) void tree_kern
     TreeState<D, NC> st;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        st.m[c] = kTreeLeast;
+        st.m[c] = kLeastMax;
         st.l[c] = 0.f;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[c][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -520,7 +517,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void tree_ring_kernel(
             qb[c][kk] = u32x4{0u, 0u, 0u, 0u};
             if (c < tiles && row < rows) qb[c][kk] = *(const u32x4*)(q + ((int64_t)(t0 + node) * Hq + g * G + head) * D + kk * 32 + (lane >> 4) * 8);
         }
-        st.m[c] = kTreeLeast;
+        st.m[c] = kLeastMax;
         st.l[c] = 0.f;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) st.o[c][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -670,7 +667,7 @@ __global__ __launch_bounds__(4 * D) void tree_merge_kernel(
     if (c >= blocks.tiles) return;
     const int32_t r = (int32_t)threadIdx.x / (D / 4), d = ((int32_t)threadIdx.x - r * (D / 4)) * 4, row = (it.block * blocks.tiles + c) * 16 + r;
     if (row >= rows) return;
-    float M = kTreeLeast, L = 0.f;
+    float M = kLeastMax, L = 0.f;
     f32x4 O = {0.f, 0.f, 0.f, 0.f};
     const int64_t at = ((int64_t)merges.e[merge].item * Hkv + g) * part_rows + c * 16 + r, next = (int64_t)blocks.blocks * Hkv * part_rows;
     // eight pieces' loads in flight at once; with more of them the maxima are read twice

@@ -914,3 +914,47 @@ def test_keys_infinitely_far_weigh_nothing(Hq, Hkv, D, ctx, new, first, end, pag
         infinitely_far(w, s, first[s], end[s], value)
     masks = [draft.ancestors(random_tree(w.rng, n, 4)) for n in new]
     near_without(w, q, Hq, masks, 2.0, run_tree(w, q, Hq, masks, 2.0), first, end)
+
+
+@pytest.mark.parametrize("dtype,value", NEGATIVE)
+@pytest.mark.parametrize("page_size", [16, 8])
+@pytest.mark.parametrize("Hq,Hkv,D,ctx,new,first,end", [
+    (4, 2, 64, (400, 300, 5), (1, 1, 1), (0, 0, 0), (200, 160, 5)),
+    (16, 2, 128, (400, 77), (1, 1), (0, 3), (390, 70)),
+    (4, 2, 128, (20000, 3), (1, 1), (0, 0), (15000, 2)),          # whole pieces
+    (4, 2, 128, (400, 300), (1, 1), (0, 0), (200, 300)),          # nothing but the token itself is left
+    (4, 2, 128, (400, 900, 300), (1, 1, 40), (0, 20, 0), (200, 880, 0)),   # beside a chunk
+])
+def test_decode_gives_keys_infinitely_far_no_weight(Hq, Hkv, D, ctx, new, first, end, page_size, dtype, value):
+    w = World(ctx, new, Hkv, D, 94, dtype, page_size)
+    q = tree_step(w, Hq, w.rng)
+    q[..., 0] = q[..., 0].abs() + 1.5
+    for s in range(len(ctx)):
+        infinitely_far(w, s, first[s], end[s], value)
+    pool, _ = w.device_pool()
+    batch, out = w.batch(), torch.full_like(q, 9.0).cuda()
+    fn("cs_paged_attention_mixed", dtype)(pool, 0, batch, q.cuda(), out, Hq, 2.0, cs.workspace_for(batch, Hq, Hkv, D))
+    w.ctx, w.new = ([x for x, n in zip(y, new) if n == 1] for y in (ctx, new))   # (the chunk's Q is scaled before it is rounded: a bound of its own)
+    near_without(w, q, Hq, None, 2.0, out.cpu(), first, end)
+
+
+@pytest.mark.parametrize("Hq,D,ctx", [(4, 64, (400, 192)), (16, 128, (400, 250)), (4, 128, (20000, 192))])
+def test_decode_over_8_bits_gives_keys_infinitely_far_no_weight(Hq, D, ctx):
+    """Codes hold no infinity: K near the greatest bf16, whose products with q are below the least float."""
+    import test_gpu_kv8
+    w, first = test_gpu_kv8.World(ctx, [1] * len(ctx), 2, D, 97), 192
+    cu = np.concatenate([[0], np.cumsum(ctx)]).astype(np.int32)
+    k, v = w.rows(int(cu[-1])), w.rows(int(cu[-1]))
+    for t in cu[:-1]:
+        k[t:t + first, :, 0] = -3.0e38
+    w.pool[:] = test_gpu_kv8.NAN_CODE
+    test_gpu_kv8.kv8.ref_append(w.pool, 0, w.tables, [0] * len(ctx), cu, k, v, 2, D)
+    _, w.pool = w.append(w.rows(w.T), w.rows(w.T))
+    q = torch.from_numpy(w.rng.standard_normal((w.T, Hq, D))).to(BF16)
+    q[..., 0] = q[..., 0].abs() + 1.5
+    batch, out = w.batch(), torch.full_like(q, 9.0).cuda()
+    cs.cs_paged_attention_mixed_kv8(w.handle(torch.from_numpy(w.pool).cuda()), 0, batch, q.cuda(), out, Hq, 0.5, cs.workspace_for_kv8(batch, Hq, 2, D))
+    for s, c in enumerate(ctx):
+        K, V = (x[first:] for x in test_gpu_kv8.kv8.read_logical(w.pool, 0, w.tables[s], c + 1, 2, D))
+        want, tol = draft.ref_tree_attention(q[s:s + 1].double().numpy(), K, V, np.ones((1, 1), bool), 0.5, HALF_STEP[BF16], False)
+        near(out[s:s + 1].cpu().double().numpy(), want, tol, (s, c))
