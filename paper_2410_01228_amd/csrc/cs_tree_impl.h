@@ -123,13 +123,14 @@ __device__ __forceinline__ void tree_scores(const TreeKv<D>& r, const u32x4 (*q)
 template <int D, class E, int NC>
 __device__ __forceinline__ u32x4 tree_weights(TreeState<D, NC>& st, int c, const float (&x)[8], float scale_log2e)
 {
-    // The maximum moves only when a score lies 2^6 above it, and only then do the lanes of a row look at each other's scores.
+    // A row's maximum moves only when a score of its own lies 2^6 above it, and only then do the lanes of a row look at each other's scores.  (The rows
+    // beside it, which look too, keep theirs: what they do not see changes no bit of them.)
     const float mine = max8(x);
     if (__any(__builtin_fmaf(mine, scale_log2e, -st.m[c]) > kTreeSlack)) {
         float mx = mine * scale_log2e;
         mx = xor_max(mx, 16);
         mx = xor_max(mx, 32);
-        const float m_new = fmaxf(st.m[c], mx);
+        const float m_new = mx - st.m[c] > kTreeSlack ? mx : st.m[c];
         const float alpha = exp2f(st.m[c] - m_new);              // 0 where nothing was seen before
         st.l[c] *= alpha;
 #pragma unroll

@@ -958,3 +958,35 @@ def test_decode_over_8_bits_gives_keys_infinitely_far_no_weight(Hq, D, ctx):
         K, V = (x[first:] for x in test_gpu_kv8.kv8.read_logical(w.pool, 0, w.tables[s], c + 1, 2, D))
         want, tol = draft.ref_tree_attention(q[s:s + 1].double().numpy(), K, V, np.ones((1, 1), bool), 0.5, HALF_STEP[BF16], False)
         near(out[s:s + 1].cpu().double().numpy(), want, tol, (s, c))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("Hq,Hkv,D,ctx,new", [
+    (4, 2, 64, (70, 0, 133), (8, 6, 5)), (16, 2, 128, (70, 200), (4, 3)), (8, 2, 64, (70, 0), (40, 30)), (8, 2, 128, (100, 260), (70, 100)), (8, 1, 128, (6000,), (60,)), (4, 2, 64, (5000,), (8,)),
+])
+def test_keys_that_a_row_does_not_see_change_no_bit_of_it(Hq, Hkv, D, ctx, new, dtype):
+    """Nodes whose K lies far out, finite or infinite in one feature: their descendants' scores climb, and rows beside them in the same tile stay as they were."""
+    w = World(ctx, new, Hkv, D, 95, dtype)
+    q = tree_step(w, Hq, w.rng, 2.0)
+    masks = [draft.ancestors(random_tree(w.rng, n, 6)) for n in new]
+    scale = 0.7 * D ** -0.5
+    clean, tables, pool = run_tree(w, q, Hq, masks, scale), w.tables, w.pool.copy()
+    apart = 0
+    for node in range(1, max(new), 3):
+        for what in ("large", "infinite"):
+            w.pool = pool.copy()
+            for s, n in enumerate(new):
+                if node < n:
+                    at = ctx[s] + node
+                    block, index = w.pool[0, tables[s, at // 16], 0], kv_layout.k_index(at % 16, np.arange(D), D)
+                    if what == "large":
+                        block[:, index] = bits(tensor(block[:, index], dtype) * 30)
+                    else:
+                        block[:, index[3]] = 0x7F80 if dtype == BF16 else 0x7C00
+            got = run_tree(w, q, Hq, masks, scale)
+            for s, n in enumerate(new):
+                for i in range(n):
+                    if node >= n or not masks[s][i, node]:
+                        assert torch.equal(got[int(w.cu[s]) + i], clean[int(w.cu[s]) + i]), (node, what, s, i)
+                        apart += 1
+    assert apart >= sum(new)                                      # (there were such rows)
