@@ -585,7 +585,12 @@ def run_layers_workspace_for(batch: Batch, num_online_seqs: int, Hq: int, Hkv: i
 # What the calls below take as bare addresses: contiguous, and as long as the kernels read or write.  (Each question to a
 # tensor costs the host 0.1 us of a call's nine, so no more are asked than a mistake could answer wrongly in silence.)
 def _rows(t: torch.Tensor, n: int) -> int:
-    assert t.is_contiguous() and t.numel() >= n
+    assert t.element_size() == 2 and t.is_contiguous() and t.numel() >= n
+    return t.data_ptr()
+
+
+def _typed_rows(t: torch.Tensor, n: int, dtype) -> int:
+    assert t.dtype is dtype and t.is_contiguous() and t.numel() >= n
     return t.data_ptr()
 
 
@@ -671,6 +676,9 @@ def compact_workspace_for(space: PageSpace, device="cuda") -> torch.Tensor:
     return torch.empty(int(lib().cs_kv_pages_compact_workspace_bytes(space.c.num_pages)), dtype=torch.uint8, device=device)
 
 
+_16_BITS = (torch.bfloat16, torch.float16)
+
+
 class Rope:
     """A cs_rope; keeps its tensors alive.  inv_freq: float32 [rotary_dim / 2]; positions: int32 [tokens] or [axes, tokens] (None: the
     batch's own, for cs_kv_append_rope); axis_pairs: pairs of each axis, where there are several; q_norm, k_norm: weights [head_dim]."""
@@ -681,57 +689,56 @@ class Rope:
             positions = positions[None]
         assert inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and 2 * inv_freq.numel() >= rotary_dim)
         assert positions is None or (positions.dtype == torch.int32 and positions.dim() == 2 and (positions.shape[1] <= 1 or positions.stride(1) == 1))
-        assert all(w is None or (w.is_contiguous() and w.element_size() == 2) for w in (q_norm, k_norm))
+        weights = [w for w in (q_norm, k_norm) if w is not None]
+        assert all(w.is_contiguous() and w.dtype in _16_BITS and w.dtype is weights[0].dtype for w in weights)
         axes = 1 if positions is None else int(positions.shape[0])
         assert axes == 1 or len(axis_pairs) == axes
         self.tensors = (inv_freq, positions, q_norm, k_norm)
         # how many tokens and features the tensors have entries for
         self.most_tokens = 2 ** 31 if positions is None else int(positions.shape[1])
-        self.most_features = min([2 ** 31] + [w.numel() for w in (q_norm, k_norm) if w is not None])
+        self.most_features = min([2 ** 31] + [w.numel() for w in weights])
+        self.types = (weights[0].dtype,) if weights else _16_BITS     # of the rows that it can be used on
         pairs = (ctypes.c_int32 * 3)(*([int(n) for n in axis_pairs] + [0] * (3 - axes) if axes > 1 else (rotary_dim // 2, 0, 0)))
         self.c = cs_rope(_ptr(inv_freq), rotary_dim, int(bool(interleaved)), _ptr(positions), 0 if positions is None or axes == 1 else positions.stride(0), axes, pairs,
                          _ptr(q_norm), _ptr(k_norm), eps)
         self.at = ctypes.addressof(self.c)
 
 
-_16_BITS = (torch.bfloat16, torch.float16)
-
-
-def _head_rows(t: torch.Tensor, tokens: int, heads: int, D: int):
+def _head_rows(t: torch.Tensor, tokens: int, heads: int, D: int, dtype):
     """(address, elements between tokens) of a [tokens, heads, D] tensor whose tokens may lie apart."""
     n, h, d = t.shape
     step, b, c = t.stride()
-    assert n >= tokens and h == heads and d == D and (b == D or h == 1) and c == 1 and t.dtype in _16_BITS
+    assert n >= tokens and h == heads and d == D and (b == D or h == 1) and c == 1 and t.dtype is dtype
     return t.data_ptr(), step if n > 1 else h * d
 
 
-def _qk_rope(fn, where, rope: Rope, q, k, q_out, k_out, stream):
+def _qk_rope(fn, where, dtype, rope: Rope, q, k, q_out, k_out, stream):
     T, Hq, D = q.shape
     Hkv = k.shape[1]
-    assert rope.most_tokens >= T and rope.most_features >= D
-    qp, qs = _head_rows(q, T, Hq, D)
-    kp, ks = _head_rows(k, T, Hkv, D)
-    rc = fn(rope.at, T, Hq, Hkv, D, qp, qs, kp, ks, _rows(q_out, T * Hq * D), _rows(k_out, T * Hkv * D), _stream(stream))
+    assert rope.most_tokens >= T and rope.most_features >= D and dtype in rope.types
+    qp, qs = _head_rows(q, T, Hq, D, dtype)
+    kp, ks = _head_rows(k, T, Hkv, D, dtype)
+    rc = fn(rope.at, T, Hq, Hkv, D, qp, qs, kp, ks, _typed_rows(q_out, T * Hq * D, dtype), _typed_rows(k_out, T * Hkv * D, dtype), _stream(stream))
     if rc:
         raise CsError(rc, where)
 
 
 def cs_qk_rope(rope: Rope, q: torch.Tensor, k: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor, stream=None):
     """q: [T, Hq, D], k: [T, Hkv, D], both possibly parts of wider rows; outputs contiguous."""
-    _qk_rope(lib().cs_qk_rope, "cs_qk_rope", rope, q, k, q_out, k_out, stream)
+    _qk_rope(lib().cs_qk_rope, "cs_qk_rope", torch.bfloat16, rope, q, k, q_out, k_out, stream)
 
 
 def cs_qk_rope_f16(rope: Rope, q: torch.Tensor, k: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor, stream=None):
-    _qk_rope(lib().cs_qk_rope_f16, "cs_qk_rope_f16", rope, q, k, q_out, k_out, stream)
+    _qk_rope(lib().cs_qk_rope_f16, "cs_qk_rope_f16", torch.float16, rope, q, k, q_out, k_out, stream)
 
 
-def _append_rope(fn, where, pool: Pool, layer, batch: Batch, rope: Rope, q, k_new, v_new, q_out, stream):
+def _append_rope(fn, where, dtype, pool: Pool, layer, batch: Batch, rope: Rope, q, k_new, v_new, q_out, stream):
     T, Hq, Hkv, D = batch.c.num_tokens, q.shape[1], pool.Hkv, pool.D
-    assert rope.most_tokens >= T and rope.most_features >= D
-    qp, qs = _head_rows(q, T, Hq, D)
-    kp, ks = _head_rows(k_new, T, Hkv, D)
-    vp, vs = _head_rows(v_new, T, Hkv, D)
-    rc = fn(pool.at, layer, batch.at, rope.at, Hq, qp, qs, kp, ks, vp, vs, _rows(q_out, T * Hq * D), _stream(stream))
+    assert rope.most_tokens >= T and rope.most_features >= D and dtype in rope.types
+    qp, qs = _head_rows(q, T, Hq, D, dtype)
+    kp, ks = _head_rows(k_new, T, Hkv, D, dtype)
+    vp, vs = _head_rows(v_new, T, Hkv, D, dtype)
+    rc = fn(pool.at, layer, batch.at, rope.at, Hq, qp, qs, kp, ks, vp, vs, _typed_rows(q_out, T * Hq * D, dtype), _stream(stream))
     if rc:
         raise CsError(rc, where)
 
@@ -739,12 +746,12 @@ def _append_rope(fn, where, pool: Pool, layer, batch: Batch, rope: Rope, q, k_ne
 def cs_kv_append_rope(pool: Pool, layer: int, batch: Batch, rope: Rope, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, q_out: torch.Tensor,
                       stream=None):
     """q: [T, Hq, D], k_new, v_new: [T, Hkv, D], possibly parts of wider rows; q_out contiguous."""
-    _append_rope(lib().cs_kv_append_rope, "cs_kv_append_rope", pool, layer, batch, rope, q, k_new, v_new, q_out, stream)
+    _append_rope(lib().cs_kv_append_rope, "cs_kv_append_rope", torch.bfloat16, pool, layer, batch, rope, q, k_new, v_new, q_out, stream)
 
 
 def cs_kv_append_rope_f16(pool: Pool, layer: int, batch: Batch, rope: Rope, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, q_out: torch.Tensor,
                           stream=None):
-    _append_rope(lib().cs_kv_append_rope_f16, "cs_kv_append_rope_f16", pool, layer, batch, rope, q, k_new, v_new, q_out, stream)
+    _append_rope(lib().cs_kv_append_rope_f16, "cs_kv_append_rope_f16", torch.float16, pool, layer, batch, rope, q, k_new, v_new, q_out, stream)
 
 
 def cs_paged_attention_tree_workspace_bytes(batch: Batch, Hq: int, Hkv: int, D: int) -> int:
@@ -755,7 +762,7 @@ def workspace_for_tree(batch: Batch, Hq: int, Hkv: int, D: int, device="cuda") -
     return torch.empty(max(cs_paged_attention_tree_workspace_bytes(batch, Hq, Hkv, D), 16), dtype=torch.uint8, device=device)
 
 
-def _tree(fn, where, pool: Pool, layer, batch: Batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream):
+def _tree(fn, where, dtype, pool: Pool, layer, batch: Batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream):
     T = batch.c.num_tokens
     n, mask, words = T * Hq * pool.D, None, 0
     if tree_mask is not None:
@@ -763,7 +770,7 @@ def _tree(fn, where, pool: Pool, layer, batch: Batch, q, out, Hq, softmax_scale,
         assert rows >= T and tree_mask.element_size() == 8 and tree_mask.is_contiguous()
         mask = tree_mask.data_ptr()
     ws, wb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    rc = fn(pool.at, layer, batch.at, _rows(q, n), _rows(out, n), Hq, softmax_scale, mask, words, ws, wb, _stream(stream))
+    rc = fn(pool.at, layer, batch.at, _typed_rows(q, n, dtype), _typed_rows(out, n, dtype), Hq, softmax_scale, mask, words, ws, wb, _stream(stream))
     if rc:
         raise CsError(rc, where)
 
@@ -771,12 +778,12 @@ def _tree(fn, where, pool: Pool, layer, batch: Batch, q, out, Hq, softmax_scale,
 def cs_paged_attention_tree(pool: Pool, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor, Hq: int, softmax_scale: float,
                             tree_mask: Optional[torch.Tensor], workspace: Optional[torch.Tensor], stream=None):
     """tree_mask: int64 [T, words] (bit j % 64 of word j / 64: node j is seen), or None: chains."""
-    _tree(lib().cs_paged_attention_tree, "cs_paged_attention_tree", pool, layer, batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream)
+    _tree(lib().cs_paged_attention_tree, "cs_paged_attention_tree", torch.bfloat16, pool, layer, batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream)
 
 
 def cs_paged_attention_tree_f16(pool: Pool, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor, Hq: int, softmax_scale: float,
                                 tree_mask: Optional[torch.Tensor], workspace: Optional[torch.Tensor], stream=None):
-    _tree(lib().cs_paged_attention_tree_f16, "cs_paged_attention_tree_f16", pool, layer, batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream)
+    _tree(lib().cs_paged_attention_tree_f16, "cs_paged_attention_tree_f16", torch.float16, pool, layer, batch, q, out, Hq, softmax_scale, tree_mask, workspace, stream)
 
 
 def cs_spec_verify_workspace_bytes(num_seqs: int, vocab: int) -> int:

@@ -277,3 +277,38 @@ def test_what_lds_is_read_by_sixteen_bytes_is_aligned_to_them(tmp_path):
     run = subprocess.run([shutil.which("hipcc") or "/opt/rocm/bin/hipcc", "--offload-arch=gfx950", "-std=c++17", "-fsyntax-only", "--cuda-host-only", "-I", os.path.join(ROOT, "include"), "-I", csrc,
                           str(source)], capture_output=True, text=True)
     assert run.returncode == 0, run.stderr
+
+
+@pytest.mark.parametrize("f16", [False, True])
+def test_binding_refuses_tensors_of_another_type(f16):
+    """Rows of the other 16-bit type would be read as other bits, and outputs of one byte an element written past their end."""
+    mine, other = (torch.float16, torch.bfloat16) if f16 else (torch.bfloat16, torch.float16)
+    fn = lambda name: getattr(cs, name + ("_f16" if f16 else ""))  # noqa: E731
+    rows = lambda h, t: torch.zeros(7, h, 64, dtype=t)  # noqa: E731
+    pool = cs.Pool.empty(1, 4, 2, 64, device="cpu")
+    batch = cs.Batch(torch.arange(4, dtype=torch.int32).view(2, 2), torch.tensor([3, 0]), torch.tensor([0, 2, 7]), device="cpu")
+    inv, norm = torch.ones(32), torch.ones(64, dtype=mine)
+    rope = cs.Rope(inv, 64, torch.arange(7, dtype=torch.int32), q_norm=norm, k_norm=norm)
+    for bad in (other, torch.float32, torch.uint8, torch.int16):
+        for i in range(4):
+            args = [rows(h, bad if i == j else mine) for j, h in enumerate((4, 2, 4, 2))]
+            with pytest.raises(AssertionError):
+                fn("cs_qk_rope")(rope, *args)
+            args = [rows(h, bad if i == j else mine) for j, h in enumerate((4, 2, 2, 4))]
+            with pytest.raises(AssertionError):
+                fn("cs_kv_append_rope")(pool, 0, batch, rope, *args)
+        for i in range(2):
+            q, out = (rows(4, bad if i == j else mine) for j in range(2))
+            with pytest.raises(AssertionError):
+                fn("cs_paged_attention_tree")(pool, 0, batch, q, out, 4, 0.1, None, None)
+        for weights in ((norm.to(bad), norm), (norm, norm.to(bad)), (norm.to(bad), norm.to(bad)), (None, norm.to(bad))):
+            with pytest.raises(AssertionError):
+                fn("cs_qk_rope")(cs.Rope(inv, 64, torch.arange(7, dtype=torch.int32), q_norm=weights[0], k_norm=weights[1]), rows(4, mine), rows(2, mine), rows(4, mine), rows(2, mine))
+    # the calls over 8 bits take either type's rows, and no shorter elements
+    pool8 = cs.Pool8.empty(1, 4, 2, 64, device="cpu")
+    for i in range(2):
+        for bad in (torch.uint8, torch.float32):
+            with pytest.raises(AssertionError):
+                fn("cs_kv8_append")(pool8, 0, batch, *(rows(2, bad if i == j else mine) for j in range(2)))
+            with pytest.raises(AssertionError):
+                fn("cs_paged_attention_mixed_kv8")(pool8, 0, batch, *(rows(4, bad if i == j else mine) for j in range(2)), 4, 0.1, None)
