@@ -990,3 +990,32 @@ def test_keys_that_a_row_does_not_see_change_no_bit_of_it(Hq, Hkv, D, ctx, new, 
                         assert torch.equal(got[int(w.cu[s]) + i], clean[int(w.cu[s]) + i]), (node, what, s, i)
                         apart += 1
     assert apart >= sum(new)                                      # (there were such rows)
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("vocab", [65536, 65537, 128256, 151936, 1 << 20])
+def test_verification_of_long_rows(vocab, drawn):
+    """More than 64 blocks of 1024 elements: draws that fall into every group of 64 and on their borders, rows that have something in one group only, and
+    random numbers that no running sum passes."""
+    groups = -(-vocab // 65536)
+    d = Drafts([2] * 7, vocab, drawn, 96, sharp=1.0)
+    d.u_next[:] = [0.0, 0.02, 0.51, 0.97, 1.0 - 2.0 ** -24, 1.0, 3.0]
+    d.run()
+    d.u[:] = 2.0                                                  # every draft is refused
+    d.run()
+    # a few elements, of weights that are exact, on both sides of the groups' borders
+    at = sorted({x for g in range(groups + 1) for x in (65536 * g - 1024, 65536 * g - 1, 65536 * g, 65536 * g + 1023) if 0 <= x < vocab} | {0, vocab - 1})
+    d.p[:], d.q[:] = 0.0, 0.0
+    d.q[:, 5] = 1.0
+    d.p[:, at] = 1.0 / 64
+    d.tokens[:] = 5
+    d.u_next[:] = [0.0, *((np.arange(1, 6) * len(at) // 6 + 0.0) / len(at)), 1.0 - 2.0 ** -24]
+    d.run()
+    for only in at[::5] + [vocab - 1]:                            # all of it at one place
+        d.p[:] = 0.0
+        d.p[:, only] = 0.5
+        d.u_next[:] = [0.0, 0.3, 0.5, 0.9, 1.0, 2.0, 0.1]
+        args = d.device()
+        cs.cs_spec_verify(*args)
+        d.check(args)
+        assert args[7][:14:2].tolist() == [only] * 7
