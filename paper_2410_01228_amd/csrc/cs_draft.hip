@@ -47,7 +47,7 @@ struct VerifyArgs {
 
 struct VerifyLds {
     double sums[kMaxRowBlocks];
-    double c, z, total;
+    double c;
     int32_t node, last, done, len, refused;                      // where the walk stands, the child tried last, whether no child is left; path's length
     int32_t path[CS_MAX_TREE], gone[CS_MAX_TREE];                // gone: tokens of refused guesses
     int32_t merges, next;
@@ -142,7 +142,7 @@ __device__ __forceinline__ void walk(const Nodes& d, VerifyLds& s, int32_t node,
             }
         }
     }
-    if (lane == 0) { s.node = node; s.last = last; s.c = c; s.z = z; s.done = done; s.len = len; s.refused = refused; }
+    if (lane == 0) { s.node = node; s.last = last; s.c = c; s.done = done; s.len = len; s.refused = refused; }
 }
 
 // A lane's 16 elements of the 1024 from base on, 256 k + 4 lane .. + 3, of a row's p and q; zeros behind its end.  No branch stands between
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyArgs
             const bool done = s.done != 0, ends = done && (total > 0.0 || whole);
             int32_t next = 0;
             if (ends) next = draw_next<kDrawn>(a, s, p, q, s.c, total, a.u_next[seq], lane);
-            if (lane == 0) { s.total = total; s.merges = ends; s.next = next; }
+            if (lane == 0) { s.merges = ends; s.next = next; }
             if (!done) walk<kDrawn>(d, s, s.node, s.last, s.c, total, s.len, lane);
             else if (!ends && lane == 0) { s.c = 0.0; s.refused = 0; }
             if (done) whole = true;
