@@ -89,7 +89,7 @@ __device__ __forceinline__ void load_nodes(const VerifyArgs& a, int32_t t0, Node
 
 // What is left of an element.  One that is negative or no number counts as nothing: of p the last maximum sees to it, since c and what counts of q are
 // not negative; q has one of its own.  (After the conversion: the maximum of a loaded float takes two instructions, the first for signalling
-// NaN.  16 drawn trees of 32, 128256 probabilities: 44.4 us with those for both, 40.0 so, 38.8 without any.)
+// NaN.  16 drawn trees of 32, 128256 probabilities, 39 us: those for both cost 5.6 us, this one 1.2.)
 template <bool kDrawn>
 __device__ __forceinline__ double left_of(float p, float q, double c) {
     if (!kDrawn) return fmax((double)p, 0.0);
@@ -204,7 +204,7 @@ __device__ __forceinline__ void drop_refused(const VerifyLds& s, int32_t base, f
 }
 
 // Sum over the wavefront, in every lane: within rows of 16 lanes by DPP, across them by swaps.  Shuffles go through LDS, six trips one
-// behind the other: 38 against 35 us for 128 chains, 52 against 47 for 4 drawn trees.
+// behind the other: 38 against 35 us for 128 chains of 6, 128256 probabilities, when those were measured.
 __device__ __forceinline__ double wave_sum(double v) {
     auto word = [](double x, int i) { return (int)(__builtin_bit_cast(uint64_t, x) >> 32 * i); };
     auto join = [](uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); };
@@ -249,36 +249,22 @@ __device__ __forceinline__ double lane_of(double v, int32_t lane) {
     return __builtin_bit_cast(double, (uint64_t)(uint32_t)lane_of((int32_t)(w >> 32), lane) << 32 | (uint64_t)(uint32_t)lane_of((int32_t)(uint32_t)w, lane));
 }
 
-// Sums of the blocks first, first + step, .. below end, by one wavefront; `take(block, sum)` gets them.  With drafts the next block is on its
-// way while one is summed: a node's refused children are passes by one workgroup, where nothing else hides the trip (4 trees of 64: 74 us
-// without, 47 with).  Guesses have no such passes, and a block at a time is 1 us less for their short rows.
+// Sums of the blocks first, first + step, .. below end, by one wavefront; `take(block, sum)` gets them.  (The next block on its way while one is
+// summed: 4 drawn trees of 64, 128256 probabilities, 34.0 us where this takes 32.4, 128 drawn chains of 6 31.9 and 30.8; of 16 drawn batches one, of a single
+// tree over 2^20 probabilities, gained 2%.)
 template <bool kDrawn, class Take>
 __device__ __forceinline__ void block_sums(const VerifyLds& s, const float* p, const float* q, double c, int32_t first, int32_t step, int32_t end, int32_t vocab, int lane, Take take)
 {
-    float x[2][4][4], y[2][4][4];
-    auto load = [&](int32_t b, float (&xx)[4][4], float (&yy)[4][4]) { load_block<kDrawn>(p, q, b * kRowBlock, vocab, xx, yy, lane); };
-    auto sum = [&](int32_t b, float (&xx)[4][4], float (&yy)[4][4]) {
-        if (!kDrawn) drop_refused(s, b * kRowBlock, xx, lane);
+    for (int32_t b = first; b < end; b += step) {
+        float x[4][4], y[4][4];
+        load_block<kDrawn>(p, q, b * kRowBlock, vocab, x, y, lane);
+        if (!kDrawn) drop_refused(s, b * kRowBlock, x, lane);
         double v = 0.0;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v += left_of<kDrawn>(xx[k][e], yy[k][e], c);
+            for (int e = 0; e < 4; ++e) v += left_of<kDrawn>(x[k][e], y[k][e], c);
         take(b, wave_sum(v));
-    };
-    if (!kDrawn) {
-        for (int32_t b = first; b < end; b += step) { load(b, x[0], y[0]); sum(b, x[0], y[0]); }
-        return;
-    }
-    if (first >= end) return;
-    load(first, x[0], y[0]);
-    for (int32_t b = first;;) {
-        if (b + step < end) load(b + step, x[1], y[1]);
-        sum(b, x[0], y[0]);
-        if ((b += step) >= end) break;
-        if (b + step < end) load(b + step, x[0], y[0]);
-        sum(b, x[1], y[1]);
-        if ((b += step) >= end) break;
     }
 }
 
