@@ -540,7 +540,8 @@ int cs_kv_append_rope_f16(const cs_kv_pool* pool, int32_t layer, const cs_batch*
  * in K or V of a key that a row does not see has no effect on it, infinities and NaN among it.  Bits of nodes that the
  * sequence does not have are not looked at.  Everything else is as in cs_paged_attention_mixed (a single token is a tree of
  * one node); chunks of more than CS_MAX_TREE tokens, and positions from 2^31 - 4096 on (here, in
- * cs_kv_append_rope and in cs_kv_tree_commit), are CS_ERR_UNSUPPORTED.  workspace: at least
+ * cs_kv_append_rope and in cs_kv_tree_commit), are CS_ERR_UNSUPPORTED: a step that also brings prompt chunks appends all of it in one
+ * call, and makes a batch of the trees and one of the chunks for the attention calls (each has its part of q and out).  workspace: at least
  * cs_paged_attention_tree_workspace_bytes(), 0 for many batches; contents are scratch, and calls that overlap in
  * time need one each. */
 size_t cs_paged_attention_tree_workspace_bytes(const cs_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim);

@@ -36,7 +36,7 @@ static TreePlan plan_tree(const cs_batch* b, int32_t Hq, int32_t Hkv, int32_t D)
     // Pieces: the length at which a model of the launch ends first.  Workgroups of the chip's slots take the pieces in order, the longest first;
     // a step costs what it does on a full chip (measured with 512 workgroups of 4064 and 8160 keys, 8 kv heads), and a piece of a cut sequence its partial
     // result and a share of the merge.  (A fixed rule, halving from 8192 keys until there were two
-    // workgroups a CU: 705 us where this one has 543, 8 trees of 64 nodes and 8 heads on 2K-32K keys.)
+    // workgroups a CU: 705 us where this one had 543, 32 trees of 8-32 nodes, 64/8 heads, on 2K-32K keys.)
     const int32_t slots = std::max(1, device_cus() * (p.tiles == 2 && D == 128 ? 1 : 2) / Hkv);
     auto step_us = [&](const TreeBlocks& t) {
         if (p.tiles <= 2) return 1.25 * (D == 64 || p.tiles == 2 ? 0.5 : 1.0);

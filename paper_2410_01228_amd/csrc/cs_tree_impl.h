@@ -405,8 +405,8 @@ __global__ __launch_bounds__(kDecodeThreads, (tree_waves(D, NC))) void tree_kern
 // More than two column tiles: the wavefronts share the rows instead of the keys.  A step's K and V are copied into an LDS ring by
 // LDS-DMA, three steps ahead of the one that is multiplied, and every wavefront reads them from there for its one to three tiles; Q stays
 // in registers.  (With the keys dealt to the wavefronts, as above, eight tiles' outputs leave registers for one step of K and V only,
-// whose loads then wait for the step before: 8 trees of 64 nodes and
-// 8 heads on contexts of 2K-32K keys: 1173 us in that form, 543 in this one, whose copies and plan are the better for it too.)
+// whose loads then wait for the step before: 32 trees of 8-32 nodes, 64/8 heads,
+// on contexts of 2K-32K keys: 1173 us in that form, 536-549 in this one, whose copies and plan are the better for it too.)
 //
 // LDS arrangement of a step: K block of the first 16-key step, 64 bytes, K block of the second, the V blocks; each as in a page of
 // 16 tokens.  Row r = 8 * step + 4 * half + i of score tile X (Y) is token 8 * half + i (+ 4) of its step, so that over X and Y a lane group

@@ -1019,3 +1019,28 @@ def test_verification_of_long_rows(vocab, drawn):
         cs.cs_spec_verify(*args)
         d.check(args)
         assert args[7][:14:2].tolist() == [only] * 7
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_trees_beside_prompt_chunks_take_a_batch_each(dtype):
+    """A step of online trees and offline chunks: one append, the trees' attention on a prefix of the batch, the chunks' on a batch of the rest."""
+    Hq, Hkv, D, ctx, new, trees = 8, 2, 64, (70, 5, 0, 40), (12, 1, 300, 260), 2
+    w = World(ctx, new, Hkv, D, 98, dtype)
+    rope, _, _, _ = make_rope(w.rng, w.T, D, D, False, False, 1, dtype)
+    x = torch.from_numpy(w.rng.standard_normal((w.T, Hq + 2 * Hkv, D))).to(dtype).cuda()
+    pool, t = w.device_pool()
+    batch, t0 = w.batch(), int(w.cu[trees])
+    q, out = (torch.full((w.T, Hq, D), 9.0, dtype=dtype, device="cuda") for _ in range(2))
+    fn("cs_kv_append_rope", dtype)(pool, 0, batch, rope, x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], q)
+    online = batch.truncated(trees)
+    offline = cs.Batch(torch.from_numpy(w.tables[trees:]), torch.tensor(ctx[trees:]), torch.from_numpy(w.cu[trees:] - t0))
+    masks = [draft.ancestors(random_tree(w.rng, n, 3)) for n in new[:trees]] + [np.tril(np.ones((n, n), bool)) for n in new[trees:]]
+    words = torch.from_numpy(np.concatenate([draft.mask_words(m, 1) for m in masks[:trees]])).cuda()
+    with pytest.raises(cs.CsError) as refused:
+        fn("cs_paged_attention_tree", dtype)(pool, 0, batch, q, out, Hq, 0.1, None, None)
+    assert refused.value.status == cs.CS_ERR_UNSUPPORTED
+    fn("cs_paged_attention_tree", dtype)(pool, 0, online, q, out, Hq, 0.1, words, cs.workspace_for_tree(online, Hq, Hkv, D))
+    assert torch.all(out[t0:] == 9.0)
+    fn("cs_paged_attention_mixed", dtype)(pool, 0, offline, q[t0:], out[t0:], Hq, 0.1, cs.workspace_for(offline, Hq, Hkv, D))
+    w.pool = w.host_pool(t)
+    check_tree(w, q.cpu(), Hq, masks, 0.1, out.cpu())
